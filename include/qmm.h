@@ -292,6 +292,80 @@ qmm_status qmm_dequantize(const uint8_t* codes, int64_t batch, int64_t rows, int
                           const qmm_granularity* g, const float* delta, void* out, qmm_dtype out_dtype, void* stream);
 
 /*
+ * qmm_rmsnorm_quantize -- the root-mean-square norm in front of a quantized product, with the addition to the residual
+ * stream before it and steps 1 and 2 (one step size per row, i.e. per token) behind it, in one pass over the row:
+ *     h    = x + residual in binary32, then rounded to x's type (x itself without a residual)
+ *     rstd = 1 / sqrt(mean_j h_j^2 + eps)          y_j = (h_j * weight_j) * rstd     (binary32, in this order)
+ *     delta, codes = what qmm_scale and qmm_quantize give for the row y in binary32 (y is not rounded in between)
+ *   x, residual   tensors of the same extent and type, contract_axis 1, cols up to 2^22; residual may be NULL.
+ *   weight        device, cols values of weight_dtype, or NULL for ones.
+ *   eps           finite and not negative.
+ *   h_out         device, dense [batch][rows][cols] of x's type, required with a residual and not written without one; may be the memory
+ *                 of x or of the residual where that is dense (QMM_ERR_SHAPE where it is not).
+ *   y_out         device, dense, x's type: y rounded once, or NULL.  rstd_out  device, batch * rows floats, or NULL.
+ *   delta_out     device, batch * rows floats;  codes_out  device [batch][rows][cols]: an operand with per_channel = 1 and
+ *                 batch_groups = batch.  Random bits of stochastic rounding as in qmm_quantize.
+ * A row whose squares overflow binary32 has rstd 0, so y 0 and delta 1; a row with an inf or NaN has delta NaN and, in FP8, codes 0x7F.
+ * A row of zeros has codes 0 and delta 1.  cols = 0: delta 1, rstd 1 / sqrt(eps).  Uses no workspace.
+ * Other types, extents or axes: QMM_ERR_SHAPE / QMM_ERR_UNSUPPORTED / QMM_ERR_ENUM; a pointer off its element's boundary: QMM_ERR_ALIGN.
+ */
+qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor* residual, const void* weight, qmm_dtype weight_dtype, float eps,
+                                qmm_format fmt, qmm_round mode, uint64_t seed, uint64_t offset, void* h_out, void* y_out,
+                                float* rstd_out, float* delta_out, uint8_t* codes_out, void* stream);
+
+/*
+ * qmm_rmsnorm_backward -- the gradients of y = h rstd weight (the quantization behind it passes them on unchanged):
+ *     a = weight * dy,  n = h * rstd,  dx = rstd * (a - n * mean_j(a n)) + dresidual,  dw = sum over all rows of dy n
+ * dx is the gradient of x and of the residual alike.
+ *   dy, h, dresidual   tensors of one extent and type, contract_axis 1; dresidual (the gradient that reaches h past the norm) or NULL.
+ *   rstd               device, batch * rows floats, as qmm_rmsnorm_quantize wrote it.
+ *   dx_out             device, dense, their type; may be the memory of one of them where that is dense.
+ *   dw_out             device, cols floats, or NULL.  Sums in binary32 in an order fixed by the extents.
+ *   workspace          qmm_rmsnorm_backward_workspace_size(dy) bytes, 16-byte aligned; not needed without dw_out.
+ * Errors as above; without rows dw is zero.
+ */
+size_t qmm_rmsnorm_backward_workspace_size(const qmm_tensor* dy);
+qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tensor* h, const float* rstd, const void* weight, qmm_dtype weight_dtype,
+                                const qmm_tensor* dresidual, void* dx_out, float* dw_out, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* Activations of a gated feed-forward block: SiLU g / (1 + e^-g), GELU g Phi(g) with the normal distribution function Phi. */
+typedef enum { QMM_ACT_SILU = 0, QMM_ACT_GELU = 1 } qmm_activation;
+
+/*
+ * qmm_gemm_gated -- both projections of a gated feed-forward block, the activation and the product in one kernel:
+ *     g = A Bg^T,  u = A Bu^T  (each descaled as in qmm_gemm, binary32),   h = act(g) * u
+ *   a          [batch][M][K].   b   [batch][2 F][K]: the F rows of the gate's weights, then the F rows of the other projection's; its
+ *              step sizes are those of an operand of 2 F rows.  Both codes (of one family), or both BF16; operands
+ *              to be quantized on load: QMM_ERR_UNSUPPORTED.
+ *   h          device [batch][M][F] of out_dtype, rounded once.
+ *   gu         device [batch][M][2 F] of out_dtype: g and u, rounded once (h is of the unrounded ones), for
+ *              qmm_gated_backward; or NULL.
+ *   workspace  qmm_gemm_gated_workspace_size() bytes, 16-byte aligned (0: may be NULL).  K is split as in qmm_gemm where M
+ *              and F are small; the parts are added in a fixed order.
+ * e^-g and Phi are evaluated in binary32 to a few units of the last place (relative to |g| 2^-23 where e^-g is far from 1).
+ * A gate of -infinity gives NaN.  Other rules and errors as for qmm_gemm.
+ */
+size_t qmm_gemm_gated_workspace_size(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K);
+qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K,
+                          qmm_activation act, void* h, void* gu, qmm_dtype out_dtype, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * qmm_gated_backward -- the backward pass of h = act(g) * u up to the operand of the products behind it:
+ *     dg = (dh * u) * act'(g),   du = dh * act(g)        a row's results are (dg | du), 2 F values
+ * as values (for the weight gradient, whose operand is quantized along the other axis) and as codes with one step size per row
+ * (the data gradient's operand [batch][rows][2 F], per_channel = 1, batch_groups = batch): what qmm_scale and qmm_quantize give for the
+ * binary32 results.
+ *   dh [..][F], gu [..][2 F]   tensors of one type, batch and rows, contract_axis 1, 2 F up to 2^22.
+ *   dgu_out     device, dense [batch][rows][2 F], their type; or NULL.  May be gu's memory where that is dense.
+ *   delta_out, codes_out   device; both or neither NULL.  At least one of codes_out and dgu_out.
+ * Random bits of stochastic rounding as in qmm_quantize.  Errors as for qmm_rmsnorm_quantize.  Uses no workspace.
+ */
+qmm_status qmm_gated_backward(const qmm_tensor* dh, const qmm_tensor* gu, qmm_activation act, qmm_format fmt, qmm_round mode,
+                              uint64_t seed, uint64_t offset, void* dgu_out, float* delta_out, uint8_t* codes_out, void* stream);
+
+/*
  * qmm_moments -- statistics of a tensor the method looks at before choosing a format (Results section, first
  * paragraph: mean, variance, skew and kurtosis of the matrix-multiply inputs).  Estimators (the paper names none):
  * population moments about the mean,  mean = sum x / n,  m_k = sum (x - mean)^k / n  for k = 2, 3, 4;

@@ -42,7 +42,7 @@
 #include <type_traits>
 
 #include <cstdlib>
-#include "qmm_device.h"
+#include "qmm_activation.h"
 
 namespace qmm {
 struct GemmArgs {
@@ -65,6 +65,9 @@ struct GemmArgs {
     double* nsr_out;                  // NSR variant: the two folded sums
     int through;                      // the outputs go past the L2 (store_through; rule in gemm_impl)
     int stagger;                      // gemm_stream_kernel: every other workgroup of an XCD starts this many sleeps late
+    int64_t F;                        // gated products: columns of each half of B (N = 2 F), else 0; y is [batch][M][F]
+    int act;                          // gated products: the activation (qmm_activation)
+    void* gu;                         // gated products: both halves' products [batch][M][2 F], or null
 };
 
 // This file is compiled once per operand-format pair, side by side (QMM_GEMM_PART = one of the numbers below; without
@@ -175,16 +178,57 @@ template <int T> QMM_DEV void store_bf16(uint16_t* dst, const float (&v)[T])
     else *reinterpret_cast<u1u*>(dst) = u1u{pk[0]};
 }
 
+// Outputs of gated products: two neighbouring columns f, f + 1 of row m of a block (rows counted from `first`, `rows_left` of them inside
+// the matrix).
+struct GatedStore {
+    void* h; void* gu;
+    int bf16;
+    int64_t F, first, rows_left;
+    QMM_DEV void pair(int m, int64_t f, const float (&hv)[2], const float (&gv)[2], const float (&uv)[2]) const
+    {
+        if (m >= rows_left || f >= F) return;
+        const int64_t row = first + m;
+        const bool two = f + 1 < F;
+        put(h, row * F + f, hv, two);
+        if (gu) {
+            put(gu, row * 2 * F + f, gv, two);
+            put(gu, row * 2 * F + F + f, uv, two);
+        }
+    }
+    QMM_DEV void put(void* p, int64_t at, const float (&v)[2], bool two) const
+    {
+        if (bf16) {
+            if (two) store_bf16<2>(static_cast<uint16_t*>(p) + at, v);
+            else static_cast<__bf16*>(p)[at] = (__bf16)v[0];
+        } else {
+            if (two) store_f32<2>(static_cast<float*>(p) + at, v);
+            else static_cast<float*>(p)[at] = v[0];
+        }
+    }
+};
+// (v0, v1) of an even and (w0, w1) of the next odd lane become (v0, w0) and (v1, w1).
+QMM_DEV void trade(float (&v)[2], bool odd)
+{
+    constexpr int SWAP_PAIRS = 0xB1;                         // quad_perm 1, 0, 3, 2
+    const float away = odd ? v[0] : v[1];
+    const float come = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(away), SWAP_PAIRS, 0xF, 0xF, true));
+    if (odd) v[0] = come; else v[1] = come;
+}
+
 // FUSE: bit 0 / bit 1 = the A / B operand arrives as bfloat16 values and is quantized (RTNE, with its step sizes)
 // while it is staged into LDS; otherwise it arrives as 8-bit codes and is copied by LDS-DMA.
 // NWN: wavefronts along N (2 or 4): the workgroup has 2 x NWN wavefronts, NWN / 2 on every SIMD.
 // NSR: the epilogue also reads the high-precision product and accumulates, per wavefront and in binary64, the two
 // sums of the noise-to-signal ratio over the values it stores (y as rounded to the output type): sum (y - ref)^2
 // and sum ref^2, elements whose error is NaN left out as in qmm_metric.  No second pass over Y.
-template <int KIND, int FA, int FB, int TM, int TG, int NWN, int FUSE, int NSR = 0>
+// GATED: B holds two matrices of F rows, gate and up, and the output is act(A gate^T) * (A up^T).  Of the B blocks of 16 (32) columns that
+// a wavefront multiplies every other one is of `up`, the one in front of it of the same columns of `gate`: both products
+// of an output element meet in one lane, and the tile's copies, schedule and matrix work are those of the plain product.
+template <int KIND, int FA, int FB, int TM, int TG, int NWN, int FUSE, int NSR = 0, int GATED = 0>
 __global__ void __launch_bounds__(64 * kWavesM * NWN, 1)
 gemm_kernel(GemmArgs g)
 {
+    static_assert(!GATED || (FUSE == 0 && NSR == 0), "gated products take operands as they are");
     constexpr bool F8 = (KIND == KIND_F8);
     constexpr bool FUSE_A = (FUSE & 1) != 0, FUSE_B = (FUSE & 2) != 0;
     static_assert(FUSE == 0 || KIND != KIND_BF16, "only 8-bit operands are quantized on load");
@@ -234,7 +278,7 @@ gemm_kernel(GemmArgs g)
     const uint32_t gsz = min(GROUP_M, (uint32_t)g.tiles_m - first_m);
     const int64_t tile_m = __builtin_amdgcn_readfirstlane((int)(first_m + (t - grp * in_group) % gsz));
     const int64_t tile_n = __builtin_amdgcn_readfirstlane((int)((t - grp * in_group) / gsz));
-    const int64_t m0 = tile_m * BM, n0 = tile_n * BN;
+    const int64_t m0 = tile_m * BM, n0 = tile_n * (GATED ? BN / 2 : BN);      // GATED: columns are counted within a half
 
     constexpr int A_ES = FUSE_A ? 2 : 1, B_ES = FUSE_B ? 2 : 1;   // source bytes per K byte of codes
     const uint8_t* A = g.a + bidx * g.M * g.rowbytes * A_ES;
@@ -271,9 +315,22 @@ gemm_kernel(GemmArgs g)
         const int p = (wave * B_PER_WAVE + i) * 8 + (lane >> 3);
         const int c = lane_chunk_base ^ ((p >> 1) & 7);
         int64_t row = WN * (p / WN) + TILES_N * (p % R) + (p / R) % TILES_N;
-        row = n0 + row < g.N ? row : g.N - 1 - n0;
+        int64_t last = g.N - 1;
+        if constexpr (GATED) {
+            row = WN / 2 * (p / WN) + TILES_N / 2 * (p % R) + (p / R) % TILES_N / 2;
+            last = g.F - 1;
+        }
+        row = n0 + row < last ? row : last - n0;
         b_src[i] = (uint32_t)((row * g.rowbytes + c * 16) * B_ES);
     }
+    // GATED: a copied unit of 8 LDS rows lies in one block, of gate or of up
+    auto b_half = [&](int i) -> const uint8_t* {
+        if constexpr (GATED) {
+            static_assert(B_PER_WAVE * 8 == 32, "a wavefront copies two blocks of 16 rows or one of 32");
+            if (F8 ? i >= B_PER_WAVE / 2 : (wave & 1) != 0) return b_tile + g.F * g.rowbytes;
+        }
+        return b_tile;
+    };
 
     // Copy number i of this wavefront for the A (B) slab at byte k0 into ring slot `slot`.
     typedef __attribute__((address_space(3))) uint8_t* lds_ptr_t;
@@ -299,7 +356,7 @@ gemm_kernel(GemmArgs g)
     };
     auto copy_b = [&](int i, int k0, int slot) {
         const int chunk = lane_chunk_base ^ ((i * 4 + (lane >> 4)) & 7);
-        copy_unit(b_tile, b_src[i], lds_b_units + slot * B_SLOT + i * 1024,
+        copy_unit(b_half(i), b_src[i], lds_b_units + slot * B_SLOT + i * 1024,
                   lds + B_BASE + slot * B_SLOT + (wave * B_PER_WAVE + i) * 1024, chunk, k0);
     };
 
@@ -511,7 +568,7 @@ gemm_kernel(GemmArgs g)
         // copy number c of the blocks before E: the rest of B slab kt+1, then A slab kt+2
         auto copy_before_e = [&](int c) {
             if (c < NB - NB_TAIL) {
-                if constexpr (STEADY) dma16_uniform(b_tile + k1, b_src[NB_TAIL + c], lds_b_units + (b_slot ^ 1) * B_SLOT + (NB_TAIL + c) * 1024);
+                if constexpr (STEADY) dma16_uniform(b_half(NB_TAIL + c) + k1, b_src[NB_TAIL + c], lds_b_units + (b_slot ^ 1) * B_SLOT + (NB_TAIL + c) * 1024);
                 else if (more) copy_b(NB_TAIL + c, k1, b_slot ^ 1);
             } else {
                 const int i = c - (NB - NB_TAIL);
@@ -573,7 +630,7 @@ gemm_kernel(GemmArgs g)
                 for (int c = 0; c < NB_TAIL; ++c)
                     if ((c * MMAS_PER_BLOCK) / (NB_TAIL > 0 ? NB_TAIL : 1) == q) {
                         __builtin_amdgcn_sched_barrier(0);
-                        if constexpr (STEADY) dma16_uniform(b_tile + k2, b_src[c], lds_b_units + b_slot * B_SLOT + c * 1024);
+                        if constexpr (STEADY) dma16_uniform(b_half(c) + k2, b_src[c], lds_b_units + b_slot * B_SLOT + c * 1024);
                         else if (more2) copy_b(c, k2, b_slot);
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -596,18 +653,21 @@ gemm_kernel(GemmArgs g)
     //  32x32: a lane's register v of acc[ia][t] is row 32*ia + 8*(v/4) + 4*(l/32) + v%4, column TILES_N*(l%32) + t
     //  so for a fixed register the TILES_N accumulators of a lane are consecutive columns, and the lanes of a
     //  store instruction cover whole rows of the wavefront tile.
-    const int64_t m_base = m0 + wm * WM, n_base = n0 + wn * WN;
+    const int64_t m_base = m0 + wm * WM, n_base = n0 + wn * (GATED ? WN / 2 : WN);
     const float* da = g.da ? g.da + ((bidx / g.da_inner) % g.da_groups) * (g.da_per_channel ? g.M : 1) : nullptr;
     const float* db = g.db ? g.db + ((bidx / g.db_inner) % g.db_groups) * (g.db_per_channel ? g.N : 1) : nullptr;
     constexpr bool descale = (KIND != KIND_BF16);
     constexpr int REGS = F8 ? 4 : 16;
-    const int64_t n = n_base + TILES_N * (lane & (R - 1));     // first of this lane's TILES_N columns
+    const int64_t n = n_base + (GATED ? TILES_N / 2 : TILES_N) * (lane & (R - 1));     // first of this lane's TILES_N (TILES_N / 2) columns
     const int lane_row = F8 ? 4 * (lane >> 4) : 4 * (lane >> 5);
     float sr[TILES_N];
 #pragma unroll
     for (int tt = 0; tt < TILES_N; ++tt) {
         sr[tt] = 1.0f;
-        if constexpr (descale) sr[tt] = g.db_per_channel ? db[(n + tt) < g.N ? (n + tt) : (g.N - 1)] : db[0];
+        if constexpr (descale && GATED) {
+            const int64_t f = n + tt / 2 < g.F ? n + tt / 2 : g.F - 1;
+            sr[tt] = g.db_per_channel ? db[f + (tt & 1 ? g.F : 0)] : db[0];
+        } else if constexpr (descale) sr[tt] = g.db_per_channel ? db[(n + tt) < g.N ? (n + tt) : (g.N - 1)] : db[0];
     }
     float sa_scalar = 1.0f;
     if constexpr (descale) { if (!g.da_per_channel) sa_scalar = da[0]; }
@@ -624,6 +684,66 @@ gemm_kernel(GemmArgs g)
         return a;
     };
     auto row_in_block = [&](int r) -> int { return F8 ? lane_row + r : 8 * (r >> 2) + lane_row + (r & 3); };
+
+    if constexpr (GATED) {
+        const int64_t rows_left = g.M - m_base;
+        float sl_rows[BLOCKS_M][REGS];
+#pragma unroll
+        for (int ia = 0; ia < BLOCKS_M; ++ia)
+#pragma unroll
+            for (int r = 0; r < REGS; ++r) {
+                sl_rows[ia][r] = sa_scalar;
+                if constexpr (descale) {
+                    if (g.da_per_channel) {
+                        const int64_t m = m_base + ia * R + row_in_block(r);
+                        sl_rows[ia][r] = da[m < g.M ? m : g.M - 1];
+                    }
+                }
+            }
+        const GatedStore out{g.y, g.gu, g.y_bf16, g.F, (bidx * g.M + m_base), rows_left};
+        auto block = [&](auto act, int ia) {
+            constexpr int ACT = decltype(act)::value;
+            uint32_t raw;
+            if constexpr (TILES_N == 4) {
+#pragma unroll
+                for (int r = 0; r < REGS; ++r) {
+                    float gv[2], uv[2], hv[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        gv[q] = value(ia, r, 2 * q, sl_rows[ia][r], raw);
+                        uv[q] = value(ia, r, 2 * q + 1, sl_rows[ia][r], raw);
+                        hv[q] = activate<ACT>(gv[q]) * uv[q];
+                    }
+                    out.pair(ia * R + row_in_block(r), n, hv, gv, uv);
+                }
+            } else {
+                // one column a lane: neighbouring lanes trade, so that the even one has two columns of the first of two rows and the odd
+                // one those of the second
+                const bool odd = (lane & 1) != 0;
+#pragma unroll
+                for (int r = 0; r < REGS; r += 2) {
+                    float gv[2], uv[2], hv[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        gv[q] = value(ia, r + q, 0, sl_rows[ia][r + q], raw);
+                        uv[q] = value(ia, r + q, 1, sl_rows[ia][r + q], raw);
+                        hv[q] = activate<ACT>(gv[q]) * uv[q];
+                    }
+                    trade(gv, odd); trade(uv, odd); trade(hv, odd);
+                    out.pair(ia * R + row_in_block(r) + (odd ? 1 : 0), n - (odd ? 1 : 0), hv, gv, uv);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (g.act == QMM_ACT_SILU) {
+#pragma unroll
+            for (int ia = 0; ia < BLOCKS_M; ++ia) if (ia * R < rows_left) block(std::integral_constant<int, QMM_ACT_SILU>{}, ia);
+        } else {
+#pragma unroll
+            for (int ia = 0; ia < BLOCKS_M; ++ia) if (ia * R < rows_left) block(std::integral_constant<int, QMM_ACT_GELU>{}, ia);
+        }
+        return;
+    }
 
     double nsr_ee = 0.0, nsr_rr = 0.0;
     auto nsr_add = [&](float stored, float ref) {
@@ -2237,16 +2357,16 @@ static inline bool ensure_lds_attr(std::atomic<uint64_t>& done, const void* kern
     return true;
 }
 
-template <int KIND, int FA, int FB, int TM, int TG, int NWN, int FUSE, int NSR = 0>
+template <int KIND, int FA, int FB, int TM, int TG, int NWN, int FUSE, int NSR = 0, int GATED = 0>
 qmm_status launch_tile(GemmArgs& g, hipStream_t s)
 {
     constexpr int BM = kWavesM * 32 * TM, BN = NWN * 64 * TG;
     constexpr int LDS_BYTES = (kASlots * BM + kBSlots * BN) * kSlabBytes;
     g.tiles_m = (int)((g.M + BM - 1) / BM);
-    g.tiles_n = (int)((g.N + BN - 1) / BN);
+    g.tiles_n = (int)(GATED ? (g.F + BN / 2 - 1) / (BN / 2) : (g.N + BN - 1) / BN);
     const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.batch * g.splits;
     if (total > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;
-    auto kern = gemm_kernel<KIND, FA, FB, TM, TG, NWN, FUSE, NSR>;
+    auto kern = gemm_kernel<KIND, FA, FB, TM, TG, NWN, FUSE, NSR, GATED>;
     static std::atomic<uint64_t> lds_attr_done{0};
     if (!ensure_lds_attr(lds_attr_done, reinterpret_cast<const void*>(kern), LDS_BYTES)) return QMM_ERR_LAUNCH;
     kern<<<(unsigned)total, 64 * kWavesM * NWN, LDS_BYTES, s>>>(g);
@@ -2408,10 +2528,22 @@ qmm_status launch_fuse(GemmArgs& g, hipStream_t s)
     return launch_tile<KIND, FA, FB, 2, 1, 2, FUSE>(g, s);
 }
 
+// Gated products: the tiles of the plain product of the same size, by its rule (launch_fuse).
+template <int KIND, int FA, int FB>
+qmm_status launch_gated(GemmArgs& g, hipStream_t s)
+{
+    const int64_t big = ((g.M + 255) / 256) * ((g.F + 127) / 128) * g.batch;
+    const int64_t small = ((g.M + 127) / 128) * ((g.F + 63) / 64) * g.batch;
+    const bool narrow = g.M <= 128 || g.F <= 64;
+    if (20 * ((big + 255) / 256) <= 11 * ((small + 511) / 512) && !narrow) return launch_tile<KIND, FA, FB, 4, 1, 4, 0, 0, 1>(g, s);
+    return launch_tile<KIND, FA, FB, 2, 1, 2, 0, 0, 1>(g, s);
+}
+
 // fuse: bit 0 = A is quantized on load, bit 1 = B is
 template <int KIND, int FA, int FB>
 qmm_status launch_kind(GemmArgs& g, hipStream_t s, int fuse)
 {
+    if (g.F > 0) return launch_gated<KIND, FA, FB>(g, s);
     if constexpr (KIND == KIND_BF16) {
         return launch_fuse<KIND, FA, FB, 0>(g, s);
     } else {
@@ -2481,6 +2613,16 @@ extern "C" size_t qmm_gemm_workspace_size(const qmm_operand* a, const qmm_operan
 }
 
 namespace {
+qmm_status launch_formats(int fa, int fb, GemmArgs& g, hipStream_t s, int fuse)
+{
+    if (fa == QMM_FMT_BF16) return launch_part<PART_BF16>(g, s, 0);
+    if (fa == QMM_FMT_INT8) return launch_part<PART_INT8>(g, s, fuse);
+    if (fa == QMM_FMT_E4M3 && fb == QMM_FMT_E4M3) return launch_part<PART_E4M3_E4M3>(g, s, fuse);
+    if (fa == QMM_FMT_E4M3) return launch_part<PART_E4M3_E5M2>(g, s, fuse);
+    if (fb == QMM_FMT_E4M3) return launch_part<PART_E5M2_E4M3>(g, s, fuse);
+    return launch_part<PART_E5M2_E5M2>(g, s, fuse);
+}
+
 size_t nsr_workspace_bytes(int64_t batch, int64_t M, int64_t N)
 {
     // a pair of binary64 sums per wavefront; 128 x 128 tiles of four wavefronts are the finest partition used
@@ -2546,14 +2688,7 @@ qmm_status gemm_impl(const qmm_operand* a, const qmm_operand* b, int64_t batch, 
     const void* out = g.splits > 1 ? g.partial : y;
     const int64_t row_bytes = N * (g.splits > 1 || !g.y_bf16 ? 4 : 2);
     g.through = row_bytes % 128 == 0 && reinterpret_cast<uintptr_t>(out) % 128 == 0 && batch * M * row_bytes * g.splits <= (int64_t)64 << 20;
-    hipStream_t s = as_stream(stream);
-
-    if (bf) return launch_part<PART_BF16>(g, s, 0);
-    if (a->format == QMM_FMT_INT8) return launch_part<PART_INT8>(g, s, fuse);
-    if (a->format == QMM_FMT_E4M3 && b->format == QMM_FMT_E4M3) return launch_part<PART_E4M3_E4M3>(g, s, fuse);
-    if (a->format == QMM_FMT_E4M3) return launch_part<PART_E4M3_E5M2>(g, s, fuse);
-    if (b->format == QMM_FMT_E4M3) return launch_part<PART_E5M2_E4M3>(g, s, fuse);
-    return launch_part<PART_E5M2_E5M2>(g, s, fuse);
+    return launch_formats(a->format, b->format, g, as_stream(stream), fuse);
 }
 }  // namespace
 
@@ -2587,5 +2722,46 @@ extern "C" qmm_status qmm_gemm_nsr(const qmm_operand* a, const qmm_operand* b, i
     }
     if (!y_ref) return QMM_ERR_NULL;
     return gemm_impl(a, b, batch, M, N, K, y, y_dtype, nullptr, y_ref, out2, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t qmm_gemm_gated_workspace_size(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K)
+{
+    return 0;
+}
+
+extern "C" qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K,
+                                     qmm_activation act, void* h, void* gu, qmm_dtype out_dtype, void* workspace, size_t workspace_bytes,
+                                     void* stream)
+{
+    qmm_status st = check_operand(a);
+    if (st != QMM_OK) return st;
+    st = check_operand(b);
+    if (st != QMM_OK) return st;
+    if (act != QMM_ACT_SILU && act != QMM_ACT_GELU) return QMM_ERR_ENUM;
+    if (out_dtype != QMM_DT_BF16 && out_dtype != QMM_DT_F32) return QMM_ERR_ENUM;
+    if (batch < 0 || M < 0 || F < 0 || K < 0) return QMM_ERR_SHAPE;
+    const bool bf = a->format == QMM_FMT_BF16;
+    if (bf != (b->format == QMM_FMT_BF16)) return QMM_ERR_UNSUPPORTED;
+    if (!bf && ((a->format == QMM_FMT_INT8) != (b->format == QMM_FMT_INT8))) return QMM_ERR_UNSUPPORTED;
+    if (!bf && (!a->is_codes || !b->is_codes)) return QMM_ERR_UNSUPPORTED;
+    if (batch * M * F == 0) return QMM_OK;
+    if (!h || (!bf && (!a->delta || !b->delta))) return QMM_ERR_NULL;
+    const int64_t esz = bf ? 2 : 1;
+    if ((K * esz) % 16 != 0) return QMM_ERR_ALIGN;
+    if (K * esz > (int64_t(1) << 22)) return QMM_ERR_UNSUPPORTED;   // the kernels keep 32-bit byte offsets within a tile's rows
+    if (K > 0 && (!a->data || !b->data)) return QMM_ERR_NULL;
+    if (!aligned16(a->data) || !aligned16(b->data) || !aligned16(h) || !aligned16(gu)) return QMM_ERR_ALIGN;
+
+    GemmArgs g{};
+    g.a = static_cast<const uint8_t*>(a->data); g.b = static_cast<const uint8_t*>(b->data);
+    g.M = M; g.N = 2 * F; g.F = F; g.rowbytes = K * esz; g.batch = batch;
+    g.da = bf ? nullptr : a->delta; g.db = bf ? nullptr : b->delta;
+    g.da_groups = a->gran.batch_groups; g.db_groups = b->gran.batch_groups;
+    g.da_inner = a->gran.batch_inner > 0 ? a->gran.batch_inner : 1;
+    g.db_inner = b->gran.batch_inner > 0 ? b->gran.batch_inner : 1;
+    g.da_per_channel = a->gran.per_channel; g.db_per_channel = b->gran.per_channel;
+    g.y = h; g.gu = gu; g.y_bf16 = out_dtype == QMM_DT_BF16; g.act = act;
+    g.splits = 1;
+    return launch_formats(a->format, b->format, g, as_stream(stream), 0);
 }
 #endif  // QMM_GEMM_HAS(0)

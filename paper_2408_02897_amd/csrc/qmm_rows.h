@@ -1,0 +1,156 @@
+// Device code shared by the operators that keep a token's row in registers between a reduction over it and its output
+// (qmm_rmsnorm.hip, qmm_gated.hip): vectors of a row, reductions over the lanes that hold one, codes of computed values.
+#pragma once
+#include <algorithm>
+#include <type_traits>
+#include "qmm_encode.h"
+
+namespace qmm {
+namespace {
+
+template <typename T> QMM_DEV u32x4 load_row(const T* p, int left)          // V elements, zeros from `left` on
+{
+    if (left >= Vec<T>::V) return *reinterpret_cast<const u32x4_any*>(p);
+    return left > 0 ? Vec<T>::partial_load(p, left) : u32x4{0u, 0u, 0u, 0u};
+}
+// binary32 values -> a vector of the tensor's type, rounded to nearest even
+template <typename T> QMM_DEV u32x4 pack_row(const float* v)
+{
+    u32x4 w;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[e]);
+    } else {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        typedef float f2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2 * e], v[2 * e + 1]}, bf2));
+    }
+    return w;
+}
+template <typename T> QMM_DEV void store_row(T* p, const u32x4& w, int left)
+{
+    if (left >= Vec<T>::V) { *reinterpret_cast<u32x4_any*>(p) = w; return; }
+#pragma unroll
+    for (int e = 0; e < Vec<T>::V; ++e)
+        if (e < left) {
+            if constexpr (sizeof(T) == 4) p[e] = __uint_as_float(w[e]);
+            else p[e] = (T)(w[e >> 1] >> (16 * (e & 1)));
+        }
+}
+// V elements of a vector of either type (the norm's weights), ones where there is none
+template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int left, float (&out)[V])
+{
+#pragma unroll
+    for (int e = 0; e < V; ++e) out[e] = 1.0f;
+    if (!w || left <= 0) return;
+    if (bf16) {
+        const uint16_t* p = static_cast<const uint16_t*>(w) + c;
+        if constexpr (V == 8) {
+            const u32x4 q = load_row<uint16_t>(p, left);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = Vec<uint16_t>::at(q, e);
+        } else if (left >= V) {
+            typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+            const u32x2_any q = *reinterpret_cast<const u32x2_any*>(p);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = __uint_as_float((e & 1) ? (q[e >> 1] & 0xFFFF0000u) : (q[e >> 1] << 16));
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) if (e < left) out[e] = bf16_bits_to_f32(p[e]);
+        }
+    } else {
+        const float* p = static_cast<const float*>(w) + c;
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            const u32x4 r = load_row<float>(p + 4 * q, left - 4 * q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[4 * q + e] = __uint_as_float(r[e]);
+        }
+    }
+}
+
+// Sums and maxima over the LPR lanes that hold a row: within a wavefront by a butterfly, above 64 lanes over the workgroup (then
+// all of it) through LDS.  The order of additions is fixed.  `turn` alternates between a workgroup's rows: with two
+// sets of words one barrier a row is enough.
+template <int LPR> struct RowReduce {
+    static constexpr int WAVES = LPR > kWave ? LPR / kWave : 1;
+    struct Shared { float sum[2][WAVES]; uint32_t max[2][WAVES]; };
+    static QMM_DEV void lanes(float& s, uint32_t& m)
+    {
+#pragma unroll
+        for (int off = (LPR < kWave ? LPR : kWave) / 2; off > 0; off >>= 1) {
+            s += __shfl_xor(s, off, kWave);
+            m = max(m, (uint32_t)__shfl_xor((int)m, off, kWave));
+        }
+    }
+    static QMM_DEV void run(float& s, uint32_t& m, Shared& sh, int turn)
+    {
+        lanes(s, m);
+        if constexpr (LPR > kWave) {
+            if ((threadIdx.x & (kWave - 1)) == 0) { sh.sum[turn][threadIdx.x / kWave] = s; sh.max[turn][threadIdx.x / kWave] = m; }
+            __syncthreads();
+            s = 0.0f; m = 0u;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) { s += sh.sum[turn][k]; m = max(m, sh.max[turn][k]); }
+        }
+    }
+};
+
+// Codes of V = 4 or 8 computed values (times rho), the first of them element number g of the random stream.
+template <int V, int MODE> QMM_DEV u32x2 encode_values(const float* y, float rho, int fmt, uint64_t g, uint64_t seed)
+{
+    constexpr int Q = V / 4;
+    float t[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) t[e] = y[e] * rho;
+    uint32_t c[Q];
+    const bool whole = MODE == QMM_ROUND_STOCHASTIC && !__any((g & 3u) != 0u);
+    if (fmt == QMM_FMT_INT8) encode_quads<QMM_FMT_INT8, MODE, Q>(t, g, seed, whole, c);
+    else if (fmt == QMM_FMT_E4M3) encode_quads<QMM_FMT_E4M3, MODE, Q>(t, g, seed, whole, c);
+    else encode_quads<QMM_FMT_E5M2, MODE, Q>(t, g, seed, whole, c);
+    return u32x2{c[0], c[Q - 1]};
+}
+
+// Lanes and vectors of a row: the smallest that hold it.  f(lanes, vectors).
+constexpr int kRowLanes = 1024, kRowElements = 16384;         // the longest row held in registers
+template <typename T, typename F> void for_row_size(int64_t cols, F f)
+{
+    constexpr int V = Vec<T>::V;
+    const int64_t nvec = (cols + V - 1) / V;
+    auto run = [&](auto lpr, auto nv) { f(lpr, nv); };
+#define QMM_ROW(L, N) run(std::integral_constant<int, L>{}, std::integral_constant<int, N>{})
+    if (nvec <= 8) QMM_ROW(8, 1);
+    else if (nvec <= 16) QMM_ROW(16, 1);
+    else if (nvec <= 32) QMM_ROW(32, 1);
+    else if (nvec <= 64) QMM_ROW(64, 1);
+    else if (nvec <= 128) QMM_ROW(64, 2);
+    else if (nvec <= 256) QMM_ROW(256, 1);
+    else if (nvec <= 512) QMM_ROW(256, 2);
+    else if (nvec <= 1024) QMM_ROW(512, 2);
+    else if (nvec <= 2048) QMM_ROW(1024, 2);
+    else if constexpr (V == 4) QMM_ROW(1024, 4);
+#undef QMM_ROW
+}
+
+// ---- arguments (host)
+constexpr int64_t kMaxColumns = int64_t(1) << 22;             // as a product's K
+inline qmm_status check_rows(const qmm_tensor* t)
+{
+    if (t->dtype != QMM_DT_BF16 && t->dtype != QMM_DT_F32) return QMM_ERR_ENUM;
+    if (t->contract_axis != 1) return t->contract_axis == 0 ? QMM_ERR_UNSUPPORTED : QMM_ERR_ENUM;
+    if (t->batch < 0 || t->rows < 0 || t->cols < 0 || t->row_stride < t->cols) return QMM_ERR_SHAPE;
+    if (t->batch > 1 && t->rows > 0 && t->batch_stride < (t->rows - 1) * t->row_stride + t->cols) return QMM_ERR_SHAPE;
+    if (t->batch > 65535 || t->cols > kMaxColumns) return QMM_ERR_UNSUPPORTED;
+    return QMM_OK;
+}
+inline bool element_aligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == QMM_DT_BF16 ? 1u : 3u)) == 0; }
+inline bool same_extent(const qmm_tensor* a, const qmm_tensor* b) { return a->batch == b->batch && a->rows == b->rows && a->cols == b->cols; }
+inline bool dense(const qmm_tensor* t)
+{
+    return (t->rows <= 1 || t->row_stride == t->cols) && (t->batch <= 1 || t->batch_stride == t->rows * t->cols);
+}
+inline unsigned row_blocks(int64_t total, int per) { return (unsigned)std::min<int64_t>((total + per - 1) / per, 0x7FFFFFFF); }
+
+}  // namespace
+}  // namespace qmm

@@ -2,6 +2,7 @@
 torch is used for device memory and the current stream.  All calls go through ctypes; quantized_operand, scale_quantize, gemm
 and metric first try the native short path for plain tensors (csrc/qmm_host.cpp), which does the same with a fifth of the
 host time.  There is no CPU fallback: a missing or unloadable library raises."""
+import collections
 import ctypes
 import importlib.util
 import os
@@ -15,10 +16,12 @@ HOST_PATH = os.path.join(_HERE, "_qmm_host.so")
 INT8, E4M3, E5M2, BF16 = 0, 1, 2, 3
 DT_BF16, DT_F32 = 0, 1
 RTNE, STOCHASTIC = 0, 1
+SILU, GELU = 0, 1
 FORMATS = {"int8": INT8, "e4m3": E4M3, "e5m2": E5M2, "bf16": BF16}
 EXPORTS = ["qmm_num_scales", "qmm_scale_workspace_size", "qmm_scale", "qmm_scale_static", "qmm_quantize", "qmm_scale_quantize_workspace_size", "qmm_scale_quantize", "qmm_scale_multi_workspace_size", "qmm_scale_multi", "qmm_quantize_multi",
            "qmm_gemm_workspace_size",
-           "qmm_gemm", "qmm_gemm_nsr_workspace_size", "qmm_gemm_nsr", "qmm_metric_workspace_size", "qmm_metric", "qmm_dequantize", "qmm_moments_workspace_size", "qmm_moments", "qmm_mfma_rate", "qmm_hbm_rate", "qmm_status_string", "qmm_version"]
+           "qmm_gemm", "qmm_gemm_nsr_workspace_size", "qmm_gemm_nsr", "qmm_metric_workspace_size", "qmm_metric", "qmm_dequantize", "qmm_rmsnorm_quantize", "qmm_rmsnorm_backward_workspace_size", "qmm_rmsnorm_backward", "qmm_gemm_gated_workspace_size", "qmm_gemm_gated", "qmm_gated_backward",
+           "qmm_moments_workspace_size", "qmm_moments", "qmm_mfma_rate", "qmm_hbm_rate", "qmm_status_string", "qmm_version"]
 
 
 class QmmError(RuntimeError):
@@ -98,6 +101,12 @@ def lib():
         L.qmm_metric_workspace_size.restype = sz; L.qmm_metric_workspace_size.argtypes = [i64]
         L.qmm_metric.restype = i32; L.qmm_metric.argtypes = [vp, i32, vp, vp, i64, vp, vp, sz, vp]
         L.qmm_dequantize.restype = i32; L.qmm_dequantize.argtypes = [vp, i64, i64, i64, i32, GP, vp, vp, i32, vp]
+        L.qmm_rmsnorm_quantize.restype = i32; L.qmm_rmsnorm_quantize.argtypes = [TP, TP, vp, i32, ctypes.c_float, i32, i32, u64, u64, vp, vp, vp, vp, vp, vp]
+        L.qmm_rmsnorm_backward_workspace_size.restype = sz; L.qmm_rmsnorm_backward_workspace_size.argtypes = [TP]
+        L.qmm_rmsnorm_backward.restype = i32; L.qmm_rmsnorm_backward.argtypes = [TP, TP, vp, vp, i32, TP, vp, vp, vp, sz, vp]
+        L.qmm_gemm_gated_workspace_size.restype = sz; L.qmm_gemm_gated_workspace_size.argtypes = [OP, OP, i64, i64, i64, i64]
+        L.qmm_gemm_gated.restype = i32; L.qmm_gemm_gated.argtypes = [OP, OP, i64, i64, i64, i64, i32, vp, vp, i32, vp, sz, vp]
+        L.qmm_gated_backward.restype = i32; L.qmm_gated_backward.argtypes = [TP, TP, i32, i32, i32, u64, u64, vp, vp, vp, vp]
         L.qmm_moments_workspace_size.restype = sz; L.qmm_moments_workspace_size.argtypes = [i64]
         L.qmm_moments.restype = i32; L.qmm_moments.argtypes = [vp, i32, i64, ctypes.c_double, vp, vp, sz, vp]
         L.qmm_mfma_rate.restype = i32
@@ -382,6 +391,119 @@ def dequantize(codes, fmt, delta, per_channel=False, batch_groups=1, out_dtype=t
     _check(L.qmm_dequantize(codes.data_ptr(), b, r, k, fmt, ctypes.byref(g), delta.data_ptr(), out.data_ptr(),
                             _dtype_code(out), _stream()), "qmm_dequantize")
     return out
+
+
+# ---- around a feed-forward block: what stands in front of and between its products
+
+Normed = collections.namedtuple("Normed", "codes delta h y rstd")
+GatedGradient = collections.namedtuple("GatedGradient", "codes delta dgu")
+
+
+def _row_desc(x, shape=None, dtype=None):
+    """tensor_desc of a tensor of rows, after the checks that the library cannot make: extents and type of another tensor."""
+    assert shape is None or tuple(x.shape) == tuple(shape), f"shape {tuple(x.shape)}, not {tuple(shape)}"
+    assert dtype is None or x.dtype == dtype, f"{x.dtype}, not {dtype}"
+    return tensor_desc(x, 1)
+
+
+def _on(device, *tensors):
+    """Kernels run on the current device's stream: all tensors of a call are there."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch._C._cuda_getDevice()):
+            raise ValueError(f"a tensor on {t.device}, which is not the current GPU")
+    return device
+
+
+def _dense_out(t, shape, dtype):
+    assert t.is_contiguous() and tuple(t.shape) == tuple(shape) and t.dtype == dtype, "an output is contiguous, of its shape and type"
+    return t
+
+
+def _weight_args(weight, cols):
+    if weight is None:
+        return None, DT_F32
+    assert weight.shape == (cols,) and weight.is_contiguous(), "one weight per column"
+    return weight.data_ptr(), _dtype_code(weight)
+
+
+def rmsnorm_quantize(x, weight, fmt, residual=None, eps=1e-6, mode=RTNE, seed=0, offset=0, want_y=False, want_rstd=False, h_out=None):
+    """qmm_rmsnorm_quantize on [rows, cols] or [batch, rows, cols]: Normed(codes [batch, rows, cols], delta, h, y, rstd).  codes and delta are an
+    operand with per_channel=True and batch_groups=batch; h is x + residual (x without one), y and rstd are None unless wanted.
+    `h_out`: where h goes, e.g. the residual itself."""
+    L = lib()
+    dev = _on(x.device, x, weight, residual, h_out)
+    t = _row_desc(x)
+    r = None if residual is None else _row_desc(residual, x.shape, x.dtype)
+    w_ptr, w_type = _weight_args(weight, t.cols)
+    h = x
+    if residual is not None:
+        h = torch.empty(x.shape, dtype=x.dtype, device=dev) if h_out is None else _dense_out(h_out, x.shape, x.dtype)
+    else:
+        assert h_out is None, "without a residual h is x"
+    codes = torch.empty((t.batch, t.rows, t.cols), dtype=torch.uint8, device=dev)
+    delta = torch.empty(t.batch * t.rows, dtype=torch.float32, device=dev)
+    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_y else None
+    rstd = torch.empty(t.batch * t.rows, dtype=torch.float32, device=dev) if want_rstd else None
+    _check(L.qmm_rmsnorm_quantize(ctypes.byref(t), None if r is None else ctypes.byref(r), w_ptr, w_type, eps, fmt, mode, seed, offset,
+                                  None if r is None else h.data_ptr(), None if y is None else y.data_ptr(), None if rstd is None else rstd.data_ptr(),
+                                  delta.data_ptr(), codes.data_ptr(), _stream()), "qmm_rmsnorm_quantize")
+    return Normed(codes, delta, h, y, rstd)
+
+
+def rmsnorm_backward(dy, h, rstd, weight, dresidual=None, want_dw=True, dx_out=None):
+    """qmm_rmsnorm_backward: (dx, dw); dw is float32, or None unless wanted.  `dx_out`: where dx goes, e.g. dy itself."""
+    L = lib()
+    dev = _on(dy.device, dy, h, rstd, weight, dresidual, dx_out)
+    t, th = _row_desc(dy), _row_desc(h, dy.shape, dy.dtype)
+    r = None if dresidual is None else _row_desc(dresidual, dy.shape, dy.dtype)
+    w_ptr, w_type = _weight_args(weight, t.cols)
+    assert rstd.dtype == torch.float32 and rstd.is_contiguous() and rstd.numel() == t.batch * t.rows, "one rstd per row"
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev) if dx_out is None else _dense_out(dx_out, dy.shape, dy.dtype)
+    dw = torch.empty(t.cols, dtype=torch.float32, device=dev) if want_dw else None
+    ws, ws_ptr, ws_bytes = _scratch(L.qmm_rmsnorm_backward_workspace_size(ctypes.byref(t)) if want_dw else 0, dev)
+    _check(L.qmm_rmsnorm_backward(ctypes.byref(t), ctypes.byref(th), rstd.data_ptr(), w_ptr, w_type, None if r is None else ctypes.byref(r),
+                                  dx.data_ptr(), None if dw is None else dw.data_ptr(), ws_ptr, ws_bytes, _stream()), "qmm_rmsnorm_backward")
+    return dx, dw
+
+
+def gemm_gated(a, b, activation=SILU, out_dtype=torch.bfloat16, want_gu=False):
+    """qmm_gemm_gated on two (data, Operand) pairs as `gemm` takes them, b = ([batch, 2 F, K], Operand) with the gate's rows first:
+    h [batch, M, F], or (h, gu [batch, M, 2 F]) when want_gu."""
+    L = lib()
+    (ta, oa), (tb, ob) = a, b
+    dev = _on(ta.device, ta, tb)
+    sa, sb = ta.shape, tb.shape
+    if len(sa) == 2:
+        sa, sb = (1, *sa), (1, *sb)
+    bt, m, k = sa
+    assert len(sb) == 3 and sb[0] == bt and sb[2] == k and sb[1] % 2 == 0, "b is [batch, 2 F, K]"
+    f = sb[1] // 2
+    h = torch.empty((bt, m, f), dtype=out_dtype, device=dev)
+    gu = torch.empty((bt, m, 2 * f), dtype=out_dtype, device=dev) if want_gu else None
+    pa, pb = ctypes.byref(oa), ctypes.byref(ob)
+    ws, ws_ptr, ws_bytes = _scratch(L.qmm_gemm_gated_workspace_size(pa, pb, bt, m, f, k), dev)
+    _check(L.qmm_gemm_gated(pa, pb, bt, m, f, k, activation, h.data_ptr(), None if gu is None else gu.data_ptr(), _dtype_code(h),
+                            ws_ptr, ws_bytes, _stream()), "qmm_gemm_gated")
+    return (h, gu) if want_gu else h
+
+
+def gated_backward(dh, gu, activation=SILU, fmt=E5M2, mode=RTNE, seed=0, offset=0, want_codes=True, want_dgu=False, dgu_out=None):
+    """qmm_gated_backward on dh [.., F] and gu [.., 2 F]: GatedGradient(codes [batch, rows, 2 F], delta, dgu), None for what is not wanted.
+    codes and delta are an operand with per_channel=True and batch_groups=batch.  `dgu_out`: where dgu goes, e.g. gu itself."""
+    L = lib()
+    dev = _on(dh.device, dh, gu, dgu_out)
+    t, tg = _row_desc(dh), _row_desc(gu, (*dh.shape[:-1], 2 * dh.shape[-1]), dh.dtype)
+    codes = torch.empty((t.batch, t.rows, 2 * t.cols), dtype=torch.uint8, device=dev) if want_codes else None
+    delta = torch.empty(t.batch * t.rows, dtype=torch.float32, device=dev) if want_codes else None
+    dgu = None
+    if dgu_out is not None:
+        dgu = _dense_out(dgu_out, gu.shape, gu.dtype)
+    elif want_dgu:
+        dgu = torch.empty(gu.shape, dtype=gu.dtype, device=dev)
+    assert codes is not None or dgu is not None, "nothing is wanted"
+    _check(L.qmm_gated_backward(ctypes.byref(t), ctypes.byref(tg), activation, fmt, mode, seed, offset, None if dgu is None else dgu.data_ptr(),
+                                None if delta is None else delta.data_ptr(), None if codes is None else codes.data_ptr(), _stream()), "qmm_gated_backward")
+    return GatedGradient(codes, delta, dgu)
 
 
 MOMENT_FIELDS = ("n", "mean", "m2", "m3", "m4", "absmax", "nan_cnt", "rsv")
