@@ -178,41 +178,109 @@ template <int T> QMM_DEV void store_bf16(uint16_t* dst, const float (&v)[T])
     else *reinterpret_cast<u1u*>(dst) = u1u{pk[0]};
 }
 
-// Outputs of gated products: two neighbouring columns f, f + 1 of row m of a block (rows counted from `first`, `rows_left` of them inside
-// the matrix).
+// Outputs of gated products one by one: column f of row m of a block (rows counted from `first`, `rows_left` of them inside the matrix).
 struct GatedStore {
     void* h; void* gu;
     int bf16;
     int64_t F, first, rows_left;
-    QMM_DEV void pair(int m, int64_t f, const float (&hv)[2], const float (&gv)[2], const float (&uv)[2]) const
+    QMM_DEV void one(int m, int64_t f, float hv, float gv, float uv) const
     {
         if (m >= rows_left || f >= F) return;
         const int64_t row = first + m;
-        const bool two = f + 1 < F;
-        put(h, row * F + f, hv, two);
+        put(h, row * F + f, hv);
         if (gu) {
-            put(gu, row * 2 * F + f, gv, two);
-            put(gu, row * 2 * F + F + f, uv, two);
+            put(gu, row * 2 * F + f, gv);
+            put(gu, row * 2 * F + F + f, uv);
         }
     }
-    QMM_DEV void put(void* p, int64_t at, const float (&v)[2], bool two) const
+    QMM_DEV void put(void* p, int64_t at, float v) const
     {
-        if (bf16) {
-            if (two) store_bf16<2>(static_cast<uint16_t*>(p) + at, v);
-            else static_cast<__bf16*>(p)[at] = (__bf16)v[0];
-        } else {
-            if (two) store_f32<2>(static_cast<float*>(p) + at, v);
-            else static_cast<float*>(p)[at] = v[0];
-        }
+        if (bf16) static_cast<__bf16*>(p)[at] = (__bf16)v; else static_cast<float*>(p)[at] = v;
     }
 };
-// (v0, v1) of an even and (w0, w1) of the next odd lane become (v0, w0) and (v1, w1).
-QMM_DEV void trade(float (&v)[2], bool odd)
+// Lanes apart by BIT (1 or 2) trade halves of a 2 x 2 block: the one with the bit clear keeps x and gets the other's x for y, the other one keeps y
+// and gets that y for x.
+template <int BIT> QMM_DEV void trade(uint32_t& x, uint32_t& y, bool set)
 {
-    constexpr int SWAP_PAIRS = 0xB1;                         // quad_perm 1, 0, 3, 2
-    const float away = odd ? v[0] : v[1];
-    const float come = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(away), SWAP_PAIRS, 0xF, 0xF, true));
-    if (odd) v[0] = come; else v[1] = come;
+    constexpr int SWAP = BIT == 1 ? 0xB1 : 0x4E;             // quad_perm 1, 0, 3, 2 and 2, 3, 0, 1
+    const uint32_t ox = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, SWAP, 0xF, 0xF, true);
+    const uint32_t oy = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)y, SWAP, 0xF, 0xF, true);
+    x = set ? oy : x;
+    y = set ? y : ox;
+}
+QMM_DEV uint32_t pack_bf16(float a, float b)
+{
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2));
+}
+
+// One A block (16 or 32 rows) of a gated product's whole tile: value(r, t) is the descaled accumulator of register r, B block t (gate and up in
+// turn).  A lane holds one or two columns of four rows (16 x 16 and 32 x 32 instructions); stored like that, four bytes a lane, the
+// stores' addresses take longer than everything else in the epilogue, so the lanes of a quad trade until each has 16 (bfloat16 by the
+// 32 x 32 instructions: 8) contiguous bytes of one row: 24 instead of 96 stores a tile and wavefront.
+// h, gu: the wavefront's first row and column (gu: gate's).  Streaming stores, as the plain product's of this size (gemm_stream_kernel).
+template <bool F8, int ACT, bool BF, bool GU, typename Value> QMM_DEV void gated_block(uint8_t* h, uint8_t* gu, int64_t F, int row0, int lane, Value&& value)
+{
+    constexpr int ES = BF ? 2 : 4, QUADS = F8 ? 1 : 4, COLS = F8 ? 2 : 1;
+    const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        float v[3][4][COLS];                                 // h, g, u of four rows
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) {
+                v[1][r][c] = value(4 * q + r, 2 * c);
+                v[2][r][c] = value(4 * q + r, 2 * c + 1);
+                v[0][r][c] = activate<ACT>(v[1][r][c]) * v[2][r][c];
+            }
+        const int row = row0 + (F8 ? 4 * (lane >> 4) : 8 * q + 4 * (lane >> 5));
+#pragma unroll
+        for (int o = 0; o < (GU ? 3 : 1); ++o) {
+            const int64_t N = o == 0 ? F : 2 * F;
+            uint8_t* base = (o == 0 ? h : gu) + (o == 2 ? F * ES : 0);
+            if constexpr (F8 && !BF) {
+                // two columns of binary32: lanes trade once, two stores of 16 bytes
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    uint32_t x0 = __float_as_uint(v[o][r][0]), x1 = __float_as_uint(v[o][r][1]);
+                    uint32_t y0 = __float_as_uint(v[o][r + 1][0]), y1 = __float_as_uint(v[o][r + 1][1]);
+                    trade<1>(x0, y0, b0); trade<1>(x1, y1, b0);
+                    __builtin_nontemporal_store(u32x4{x0, x1, y0, y1}, reinterpret_cast<u32x4*>(base + ((row + r + (lane & 1)) * N + 4 * ((lane & 15) >> 1)) * ES));
+                }
+            } else if constexpr (!F8 && BF) {
+                // one column: rows in pairs to a dword, then the odd lane has the second row of a pair, then lanes 2 and 3 the second pair
+                const uint32_t pick = b0 ? 0x03020706u : 0x05040100u;
+                uint32_t d[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t own = pack_bf16(v[o][2 * k][0], v[o][2 * k + 1][0]);
+                    d[k] = __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_update_dpp(0, (int)own, 0xB1, 0xF, 0xF, true), own, pick);
+                }
+                trade<2>(d[0], d[1], b1);
+                __builtin_nontemporal_store(u32x2{d[0], d[1]}, reinterpret_cast<u32x2*>(base + ((row + (lane & 3)) * N + 4 * ((lane & 31) >> 2)) * ES));
+            } else {
+                uint32_t d[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) d[r] = F8 ? pack_bf16(v[o][r][0], v[o][r][COLS - 1]) : __float_as_uint(v[o][r][0]);
+                trade<1>(d[0], d[1], b0); trade<1>(d[2], d[3], b0);
+                trade<2>(d[0], d[2], b1); trade<2>(d[1], d[3], b1);
+                __builtin_nontemporal_store(u32x4{d[0], d[1], d[2], d[3]},
+                                            reinterpret_cast<u32x4*>(base + ((row + (lane & 3)) * N + (F8 ? 8 * ((lane & 15) >> 2) : 4 * ((lane & 31) >> 2))) * ES));
+            }
+        }
+    }
+}
+// Calls f(activation, bfloat16?, gu?) with the constants of a call.
+template <typename Fn> QMM_DEV void gated_forms(const GemmArgs& g, Fn&& f)
+{
+    using T = std::true_type; using N = std::false_type;
+    auto outputs = [&](auto act) {
+        if (g.y_bf16) { if (g.gu) f(act, T{}, T{}); else f(act, T{}, N{}); }
+        else { if (g.gu) f(act, N{}, T{}); else f(act, N{}, N{}); }
+    };
+    if (g.act == QMM_ACT_SILU) outputs(std::integral_constant<int, QMM_ACT_SILU>{}); else outputs(std::integral_constant<int, QMM_ACT_GELU>{});
 }
 
 // FUSE: bit 0 / bit 1 = the A / B operand arrives as bfloat16 values and is quantized (RTNE, with its step sizes)
@@ -700,39 +768,31 @@ gemm_kernel(GemmArgs g)
                     }
                 }
             }
-        const GatedStore out{g.y, g.gu, g.y_bf16, g.F, (bidx * g.M + m_base), rows_left};
+        uint32_t raw;
+        if (m0 + BM <= g.M && n0 + BN / 2 <= g.F && g.F % 8 == 0) {
+            const int es = g.y_bf16 ? 2 : 4;
+            uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.M + m_base) * g.F + n_base) * es;
+            uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.M + m_base) * 2 * g.F + n_base) * es;
+            gated_forms(g, [&](auto act, auto bf, auto kept) {
+#pragma unroll
+                for (int ia = 0; ia < BLOCKS_M; ++ia) {
+                    gated_block<F8, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
+                        h, gu, g.F, ia * R, lane, [&](int r, int t) { return value(ia, r, t, sl_rows[ia][r], raw); });
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            });
+            return;
+        }
+        // tiles at an edge, and rows that do not begin at a vector's boundary
+        const GatedStore out{g.y, g.gu, g.y_bf16, g.F, bidx * g.M + m_base, rows_left};
         auto block = [&](auto act, int ia) {
-            constexpr int ACT = decltype(act)::value;
-            uint32_t raw;
-            if constexpr (TILES_N == 4) {
 #pragma unroll
-                for (int r = 0; r < REGS; ++r) {
-                    float gv[2], uv[2], hv[2];
+            for (int r = 0; r < REGS; ++r)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        gv[q] = value(ia, r, 2 * q, sl_rows[ia][r], raw);
-                        uv[q] = value(ia, r, 2 * q + 1, sl_rows[ia][r], raw);
-                        hv[q] = activate<ACT>(gv[q]) * uv[q];
-                    }
-                    out.pair(ia * R + row_in_block(r), n, hv, gv, uv);
+                for (int c = 0; c < TILES_N / 2; ++c) {
+                    const float gv = value(ia, r, 2 * c, sl_rows[ia][r], raw), uv = value(ia, r, 2 * c + 1, sl_rows[ia][r], raw);
+                    out.one(ia * R + row_in_block(r), n + c, activate<decltype(act)::value>(gv) * uv, gv, uv);
                 }
-            } else {
-                // one column a lane: neighbouring lanes trade, so that the even one has two columns of the first of two rows and the odd
-                // one those of the second
-                const bool odd = (lane & 1) != 0;
-#pragma unroll
-                for (int r = 0; r < REGS; r += 2) {
-                    float gv[2], uv[2], hv[2];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        gv[q] = value(ia, r + q, 0, sl_rows[ia][r + q], raw);
-                        uv[q] = value(ia, r + q, 1, sl_rows[ia][r + q], raw);
-                        hv[q] = activate<ACT>(gv[q]) * uv[q];
-                    }
-                    trade(gv, odd); trade(uv, odd); trade(hv, odd);
-                    out.pair(ia * R + row_in_block(r) + (odd ? 1 : 0), n - (odd ? 1 : 0), hv, gv, uv);
-                }
-            }
             __builtin_amdgcn_sched_barrier(0);
         };
         if (g.act == QMM_ACT_SILU) {
@@ -1291,7 +1351,8 @@ gemm_shortk_kernel(GemmArgs g)
 // Operands as they are (codes, or bfloat16 for the reference product), whole tiles, whole slabs, no split, output in y
 // alone; same fragment, accumulator and store layout as gemm_kernel.  The reference product gains least, its 268 MB of
 // binary32 output being what it waits for: 16384 x 4096 x 1024 151 -> 147 us back to back against gemm_kernel.
-template <int KIND, int FA, int FB>
+// GATED: see gemm_kernel; the step sizes of a lane's columns are those of gate and up in turn.
+template <int KIND, int FA, int FB, int GATED = 0>
 __global__ void __launch_bounds__(512, 1)
 gemm_stream_kernel(GemmArgs g)
 {
@@ -1338,14 +1399,18 @@ gemm_stream_kernel(GemmArgs g)
     for (int i = 0; i < NB; ++i) {
         const int p = (wave * NB + i) * 8 + (lane >> 3);
         const int c = (lane & 7) ^ ((p >> 1) & 7);
-        const int row = WN * (p / WN) + TILES_N * (p % R) + (p / R) % TILES_N;
+        const int row = GATED ? WN / 2 * (p / WN) + TILES_N / 2 * (p % R) + (p / R) % TILES_N / 2 : WN * (p / WN) + TILES_N * (p % R) + (p / R) % TILES_N;
         b_src[i] = (uint32_t)(row * rowbytes + c * 16);
     }
+    const int64_t up_rows = GATED ? g.F * g.rowbytes : 0;          // from gate's rows to up's
+    auto is_up = [&](int i) -> bool { return F8 ? i >= NB / 2 : (wave & 1) != 0; };
     typedef __attribute__((address_space(3))) uint8_t* lds_ptr_t;
     const uint32_t lds_a_units = (uint32_t)(uintptr_t)(lds_ptr_t)(lds + wave * NA * 1024);
     const uint32_t lds_b_units = (uint32_t)(uintptr_t)(lds_ptr_t)(lds + B_BASE + wave * NB * 1024);
     auto copy_a = [&](const uint8_t* slab, int i, int slot) { dma16_uniform(slab, a_src[i], lds_a_units + slot * A_SLOT + i * 1024); };
-    auto copy_b = [&](const uint8_t* slab, int i, int slot) { dma16_uniform(slab, b_src[i], lds_b_units + slot * B_SLOT + i * 1024); };
+    auto copy_b = [&](const uint8_t* slab, int i, int slot) {
+        dma16_uniform(GATED && is_up(i) ? slab + up_rows : slab, b_src[i], lds_b_units + slot * B_SLOT + i * 1024);
+    };
 
     // workgroup-wide tile number -> tile, with gemm_kernel's mapping (XCD-aware, grouped along m); the tiles of one
     // workgroup (numbers blockIdx.x + i * gridDim.x, the grid a multiple of the XCD count) stay within its XCD's range
@@ -1364,7 +1429,7 @@ gemm_stream_kernel(GemmArgs g)
         const int64_t tile_m = __builtin_amdgcn_readfirstlane((int)(first_m + (t - grp * in_group) % gsz));
         const int64_t tile_n = __builtin_amdgcn_readfirstlane((int)((t - grp * in_group) / gsz));
         Tile o;
-        o.bidx = bidx; o.m0 = tile_m * BM; o.n0 = tile_n * BN;
+        o.bidx = bidx; o.m0 = tile_m * BM; o.n0 = tile_n * (GATED ? BN / 2 : BN);
         o.a = g.a + (bidx * g.M + o.m0) * g.rowbytes;
         o.b = g.b + (bidx * g.N + o.n0) * g.rowbytes;
         return o;
@@ -1547,7 +1612,11 @@ gemm_stream_kernel(GemmArgs g)
                 // E: every LDS read of this slab has completed and the next slab has landed
                 if constexpr (START) {
                     // the newest operations are the stores of the tile before; for the first tile, the copies of A slab 2
-                    if (t_cur == blockIdx.x) wait_vm_lgkm<NA>(); else wait_vm_lgkm<STORES_W>();
+                    if (t_cur == blockIdx.x) wait_vm_lgkm<NA>();
+                    else if constexpr (GATED) {                    // (gated_block's stores: 8 or 16 of h, as many of g and of u)
+                        if (F8 && g.y_bf16) { if (g.gu) wait_vm_lgkm<3 * 8>(); else wait_vm_lgkm<8>(); }
+                        else { if (g.gu) wait_vm_lgkm<3 * 16>(); else wait_vm_lgkm<16>(); }
+                    } else wait_vm_lgkm<STORES_W>();
                 } else {
                     if (more2) wait_vm_lgkm<NA>(); else wait_vm_lgkm<0>();
                 }
@@ -1589,7 +1658,7 @@ gemm_stream_kernel(GemmArgs g)
             asm volatile("" : "+v"(lane_s));
             const float* pa = g.da + (g.da_per_channel ? (int64_t)ga * g.M + cur.m0 + wm * WM + lane_s : (int64_t)ga);
             const float* pa1 = g.da_per_channel ? pa + 64 : pa;
-            const float* pb = g.db + (g.db_per_channel ? (int64_t)gb * g.N + cur.n0 + wn * WN + TILES_N * (lane_s & (R - 1)) : (int64_t)gb);
+            const float* pb = g.db + (g.db_per_channel ? (int64_t)gb * g.N + cur.n0 + wn * (GATED ? WN / 2 : WN) + (GATED ? TILES_N / 2 : TILES_N) * (lane_s & (R - 1)) : (int64_t)gb);
 #if defined(__HIP_DEVICE_COMPILE__)
             // (in-out operands: the loads write the very registers that are carried round the tile loop, so that no copy of
             // a register that has not landed yet is made behind them; build --check-asm looks for such reads)
@@ -1598,10 +1667,10 @@ gemm_stream_kernel(GemmArgs g)
             // (one register per load -- a vector's registers were copied behind the load -- and one statement whatever the
             // granularity -- registers that met behind a branch were copied there: with one step size per group the
             // lane's four loads read the same word)
-            const float* pb1 = g.db_per_channel ? pb + 1 : pb;
+            const float* pb1 = g.db_per_channel ? pb + (GATED ? g.F : 1) : pb;
             if constexpr (F8) {
-                const float* pb2 = g.db_per_channel ? pb + 2 : pb;
-                const float* pb3 = g.db_per_channel ? pb + 3 : pb;
+                const float* pb2 = g.db_per_channel ? pb + (GATED ? 1 : 2) : pb;
+                const float* pb3 = g.db_per_channel ? pb + (GATED ? g.F + 1 : 3) : pb;
                 asm volatile("global_load_dword %0, %4, off\n\tglobal_load_dword %1, %5, off\n\t"
                              "global_load_dword %2, %6, off\n\tglobal_load_dword %3, %7, off"
                              : "+v"(sc_b0), "+v"(sc_b1), "+v"(sc_b2), "+v"(sc_b3) : "v"(pb), "v"(pb1), "v"(pb2), "v"(pb3));
@@ -1632,7 +1701,7 @@ gemm_stream_kernel(GemmArgs g)
             asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
         };
-        const int64_t m_base = cur.m0 + wm * WM, n_base = cur.n0 + wn * WN;
+        const int64_t m_base = cur.m0 + wm * WM, n_base = cur.n0 + wn * (GATED ? WN / 2 : WN);
         int lane_e = lane;                    // kept out of the loop-invariant code the compiler would hoist
         asm volatile("" : "+v"(lane_e));
         const int64_t n = n_base + TILES_N * (lane_e & (R - 1));
@@ -1651,7 +1720,19 @@ gemm_stream_kernel(GemmArgs g)
         // next: measured on the benchmark's step, this kernel takes 2 (QKV) and 7 us (FFN1) longer and the metric
         // pass over the four outputs 20 us less.
         auto store_tile = [&](auto&& value) {
-            if (g.y_bf16) {
+            if constexpr (GATED) {
+                const int es = g.y_bf16 ? 2 : 4;
+                uint8_t* h = static_cast<uint8_t*>(g.y) + ((cur.bidx * g.M + m_base) * g.F + n_base) * es;
+                uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((cur.bidx * g.M + m_base) * 2 * g.F + n_base) * es;
+                gated_forms(g, [&](auto act, auto bf, auto kept) {
+#pragma unroll
+                    for (int ia = 0; ia < BLOCKS_M; ++ia) {
+                        gated_block<F8, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
+                            h, gu, g.F, ia * R, lane_e, [&](int r, int t) { return value(ia, r, t); });
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
+            } else if (g.y_bf16) {
                 uint8_t* ybase = static_cast<uint8_t*>(g.y) + ((cur.bidx * g.M + m_base) * g.N + n) * 2;
                 const int64_t row_bytes = g.N * 2;
                 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
@@ -2454,16 +2535,16 @@ bool use_stream(const GemmArgs& g, int fuse)
     return (g.M / 256) * (g.N / 256) * g.batch > kStreamGrid;
 }
 
-template <int KIND, int FA, int FB>
+template <int KIND, int FA, int FB, int GATED = 0>
 qmm_status launch_stream(GemmArgs& g, hipStream_t s)
 {
     constexpr int LDS_BYTES = (kASlots + kBSlots) * 256 * kSlabBytes;
     g.tiles_m = (int)(g.M / 256);
-    g.tiles_n = (int)(g.N / 256);
+    g.tiles_n = (int)(g.N / 256);                       // (gated: 128 of gate and 128 of up)
     if ((int64_t)g.tiles_m * g.tiles_n * g.batch > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;
     const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n * g.batch;
     g.stagger = tiles < 3 * kStreamGrid ? 0 : tiles < 4 * kStreamGrid ? 8 : 16;
-    auto kern = gemm_stream_kernel<KIND, FA, FB>;
+    auto kern = gemm_stream_kernel<KIND, FA, FB, GATED>;
     static std::atomic<uint64_t> lds_attr_done{0};
     if (!ensure_lds_attr(lds_attr_done, reinterpret_cast<const void*>(kern), LDS_BYTES)) return QMM_ERR_LAUNCH;
     kern<<<kStreamGrid, 512, LDS_BYTES, s>>>(g);
@@ -2532,6 +2613,7 @@ qmm_status launch_fuse(GemmArgs& g, hipStream_t s)
 template <int KIND, int FA, int FB>
 qmm_status launch_gated(GemmArgs& g, hipStream_t s)
 {
+    if (use_stream(g, 0)) return launch_stream<KIND, FA, FB, 1>(g, s);
     const int64_t big = ((g.M + 255) / 256) * ((g.F + 127) / 128) * g.batch;
     const int64_t small = ((g.M + 127) / 128) * ((g.F + 63) / 64) * g.batch;
     const bool narrow = g.M <= 128 || g.F <= 64;

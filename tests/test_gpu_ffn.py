@@ -247,6 +247,33 @@ def test_gated_product_in_batches(batch, m, f, k, fmt):
     near(got, h, off)
 
 
+@pytest.mark.parametrize("fa,fb", [(qmm.INT8, qmm.INT8), (qmm.E4M3, qmm.E4M3), (qmm.E5M2, qmm.E4M3), (qmm.BF16, qmm.BF16)])
+@pytest.mark.parametrize("batch,m,f,k", [(1, 2304, 3712, 384), (3, 1280, 2304, 512), (2, 4096, 1152, 640), (1, 4096, 2176, 400), (1, 2304, 3712, 256)])
+def test_gated_product_of_many_tiles(batch, m, f, k, fa, fb):
+    """Both projections are the plain product's bits; h follows from them.  Whole tiles that stay on their CU, ragged contractions, batches, every kind
+    of step sizes."""
+    x, w = normal(1, batch, m, k).to(DEV), normal(2, batch, 2 * f, k, scale=1.5 / k ** 0.5).to(DEV)
+    for per_channel, groups in ((True, batch), (False, 1), (True, 1), (False, batch)):
+        def side(t, fmt):
+            if fmt == qmm.BF16:
+                c = t.to(BF)
+                return c, qmm.operand(c, fmt, is_codes=False)
+            return qmm.quantized_operand(t, 1, fmt, per_channel=per_channel, batch_groups=groups)[0]
+        a, b = side(x, fa), side(w, fb)
+        want = qmm.gemm(a, b, F32)
+        g, u = want[..., :f].double(), want[..., f:].double()
+        for kind in (qmm.SILU, qmm.GELU):
+            value = g * torch.sigmoid(g) if kind == qmm.SILU else 0.5 * g * torch.special.erfc(-g * 0.5 ** 0.5)
+            off = ((g.abs() if kind == qmm.SILU else g * g) + 8) * 2.0 ** -22 * (value * u).abs() + 2.0 ** -126
+            for dtype in (F32, BF):
+                h, gu = qmm.gemm_gated(a, b, kind, dtype, want_gu=True)
+                assert torch.equal(gu, want.to(dtype))
+                assert torch.all((h.double() - value * u).abs() <= off + R.rounding(dtype) * ((value * u).abs() + off))
+                assert torch.equal(qmm.gemm_gated(a, b, kind, dtype), h)
+        if fa == qmm.BF16:
+            break
+
+
 @pytest.mark.parametrize("m", [1, 20, 200])
 def test_gated_product_by_scale_groups(m):
     """One step size per tensor or per group of matrices instead of per row."""
