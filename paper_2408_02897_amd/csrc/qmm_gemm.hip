@@ -38,6 +38,7 @@
 //    several whole tiles per CU and one step size per operand: gemm_stream_kernel
 //    (both: workgroups that stay on their CU and overlap a tile's stores with the
 //    next tile's work).
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -179,6 +180,7 @@ template <int T> QMM_DEV void store_bf16(uint16_t* dst, const float (&v)[T])
     else *reinterpret_cast<u1u*>(dst) = u1u{pk[0]};
 }
 
+constexpr int kGatedFew = 64;                              // tokens up to which gated_few_kernel serves
 constexpr int64_t kGatedColumns = int64_t(1) << 22;          // F up to which 64 rows of (g | u) in binary32 lie within 32-bit offsets
 
 // Gated products.  The weights are the first operand: a lane of the matrix instructions then holds several rows of a block, i.e. columns of the
@@ -288,6 +290,44 @@ QMM_DEV void gated_one(const GemmArgs& g, int64_t bidx, int64_t n, int64_t f, fl
         put(g.gu, row * 2 * g.F + g.F + f, uv);
     }
 }
+// Split contractions: raw accumulators of four neighbouring columns of gate (half 0) or up to their place in partial [split][batch][N][2 F].
+QMM_DEV void gated_part(const GemmArgs& g, int split, int64_t bidx, int64_t n, int half, int64_t f, u32x4 raw)
+{
+    if (n >= g.N || f >= g.F) return;
+    uint32_t* p = static_cast<uint32_t*>(g.partial) + ((((int64_t)split * g.batch + bidx) * g.N + n) * 2 + half) * g.F + f;
+    if (g.F % 4 == 0) { *reinterpret_cast<u32x4*>(p) = raw; return; }
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (f + v < g.F) p[v] = raw[v];
+}
+// The outputs of a split gated product: the parts added in ascending order (INT8 exactly), descaled, activated.
+template <int KIND> __global__ void __launch_bounds__(256) gated_reduce(GemmArgs g)
+{
+    const int64_t f = (int64_t)blockIdx.x * 256 + threadIdx.x, n = blockIdx.y, bidx = blockIdx.z;
+    if (f >= g.F) return;
+    const int64_t one = g.batch * g.N * 2 * g.F;             // words of a part
+    const uint32_t* p = static_cast<const uint32_t*>(g.partial) + (bidx * g.N + n) * 2 * g.F + f;
+    float gv, uv;
+    if constexpr (KIND == KIND_I8) {
+        int32_t a = 0, b = 0;
+#pragma unroll 4
+        for (int s = 0; s < g.splits; ++s) { a += (int32_t)p[s * one]; b += (int32_t)p[s * one + g.F]; }
+        gv = (float)a; uv = (float)b;
+    } else {
+        gv = 0.0f; uv = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < g.splits; ++s) { gv += __uint_as_float(p[s * one]); uv += __uint_as_float(p[s * one + g.F]); }
+    }
+    if constexpr (KIND != KIND_BF16) {
+        const float* da = g.da + ((bidx / g.da_inner) % g.da_groups) * (g.da_per_channel ? g.M : 1);
+        const float token = g.db[((bidx / g.db_inner) % g.db_groups) * (g.db_per_channel ? g.N : 1) + (g.db_per_channel ? n : 0)];
+        gv = (gv * token) * da[g.da_per_channel ? f : 0];
+        uv = (uv * token) * da[g.da_per_channel ? g.F + f : 0];
+    }
+    const float a = g.act == QMM_ACT_SILU ? activate<QMM_ACT_SILU>(gv) : activate<QMM_ACT_GELU>(gv);
+    gated_one(g, bidx, n, f, a * uv, gv, uv);
+}
+
 // Calls f(activation, bfloat16?, gu?) with the constants of a call.
 template <typename Fn> QMM_DEV void gated_forms(const GemmArgs& g, Fn&& f)
 {
@@ -792,6 +832,22 @@ gemm_kernel(GemmArgs g)
                 a = (a * sr[tt]) * __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from + (ia * R % 64 + row_in_block(v) - lane_row) * 4, sc[ia * R / 64]));
             return a;
         };
+        if (g.splits > 1) {
+#pragma unroll
+            for (int tt = 0; tt < TILES_N; ++tt)
+#pragma unroll
+                for (int ia = 0; ia < BLOCKS_M; ++ia)
+#pragma unroll
+                    for (int v = 0; v < REGS; v += 4) {
+                        bool up;
+                        const int64_t f = f_base + gated_row<F8, NP>(ia * R + row_in_block(v), up);
+                        u32x4 raw;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { uint32_t w; asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(w) : "a"(acc[ia][tt][v + e])); raw[e] = w; }
+                        gated_part(g, split, bidx, n + tt, ia & 1, f, raw);
+                    }
+            return;
+        }
         if (m0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0 && g.F <= kGatedColumns) {
             const int es = g.y_bf16 ? 2 : 4;
             gated_forms(g, [&](auto act, auto bf, auto kept) {
@@ -2363,7 +2419,9 @@ gated_few_kernel(GemmArgs g)
     const uint32_t blocks = (uint32_t)g.tiles_m;
     const int64_t bidx = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / blocks));
     const int64_t f0 = 16 * (int64_t)(blockIdx.x - (uint32_t)bidx * blocks);
-    const int rowbytes = (int)g.rowbytes, nk = (rowbytes + kSlabBytes - 1) / kSlabBytes;
+    const int rowbytes = (int)g.rowbytes, slabs = (rowbytes + kSlabBytes - 1) / kSlabBytes;
+    // this workgroup's slabs: all, or one of g.splits ranges
+    const int split = blockIdx.y, begin = (int)((int64_t)slabs * split / g.splits), nk = (int)((int64_t)slabs * (split + 1) / g.splits);
 
     const uint8_t* rows[2 + TB];                             // of gate, of up, of the tokens' blocks
     {
@@ -2412,11 +2470,11 @@ gated_few_kernel(GemmArgs g)
                 }
             }
     };
-    // this wavefront's slabs are wave, wave + W, ...: AHEAD of them at a time
+    // this wavefront's slabs are begin + wave, begin + wave + W, ...: AHEAD of them at a time
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
-        if (wave + i * W < nk) load(wave + i * W, frag[i]);
-    for (int k = wave; k < nk; k += AHEAD * W) {
+        if (begin + wave + i * W < nk) load(begin + wave + i * W, frag[i]);
+    for (int k = begin + wave; k < nk; k += AHEAD * W) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (k + i * W < nk) {
@@ -2443,6 +2501,11 @@ gated_few_kernel(GemmArgs g)
             sum[h] = sums[(t * 2 + h) * 64 + lane];
 #pragma unroll
             for (int w = 1; w < W; ++w) sum[h] += sums[((w * TB + t) * 2 + h) * 64 + lane];
+        }
+        if (g.splits > 1) {
+            gated_part(g, split, bidx, n, 0, f0 + 4 * q, __builtin_bit_cast(u32x4, sum[0]));
+            gated_part(g, split, bidx, n, 1, f0 + 4 * q, __builtin_bit_cast(u32x4, sum[1]));
+            continue;
         }
         if (n >= g.N) continue;
         const float token = db ? db[g.db_per_channel ? n : 0] : 1.0f;
@@ -2579,6 +2642,19 @@ int plan_splits(int64_t M, int64_t N, int64_t rowbytes, int64_t batch, int fuse)
     return splits >= 2 ? (int)splits : 1;
 }
 
+// The same for gated products of M tokens: 128 x 128 tiles (64 columns of both halves) as above, or, up to 64 tokens, the workgroups of 16 columns of
+// gated_few_kernel, of which a CU takes two.  The second kernel takes 3 us, so few tokens are split from 48 slabs on (E4M3, one token, unsplit / split: 512 x 8192
+// 11.5 / 7.5 us, 1000 x 2000 5.1 / 7.0; 64 tokens 1024 x 8192 25.5 / 16.8).  Its grid has the tokens and matrices for dimensions.
+int plan_gated_splits(int64_t M, int64_t F, int64_t rowbytes, int64_t batch)
+{
+    const int64_t nslabs = (rowbytes + kSlabBytes - 1) / kSlabBytes;
+    if (nslabs < (M <= kGatedFew ? 48 : 16) || M > 65535 || batch > 65535) return 1;
+    const int64_t blocks = M <= kGatedFew ? (F + 15) / 16 * batch : ((M + 127) / 128) * ((F + 63) / 64) * batch;
+    if (blocks >= 256) return 1;
+    const int64_t splits = std::min<int64_t>(512 / blocks, nslabs / 8);
+    return splits >= 2 ? (int)splits : 1;
+}
+
 // The dynamic-LDS limit of a kernel is a property of the function on one device: it is applied once per
 // (instantiation, device), the devices already served kept as a bit mask (devices past 63 are served on every call).
 // Two host threads that meet here both apply it, which is harmless; nothing else is remembered between calls.
@@ -2591,6 +2667,13 @@ static inline bool ensure_lds_attr(std::atomic<uint64_t>& done, const void* kern
     if (hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
     if (bit) done.fetch_or(bit, std::memory_order_release);
     return true;
+}
+
+template <int KIND> qmm_status launch_gated_reduce(const GemmArgs& g, hipStream_t s)
+{
+    if (hipGetLastError() != hipSuccess) return QMM_ERR_LAUNCH;
+    gated_reduce<KIND><<<dim3((unsigned)((g.F + 255) / 256), (unsigned)g.N, (unsigned)g.batch), 256, 0, s>>>(g);
+    return launch_status();
 }
 
 template <int KIND, int FA, int FB, int TM, int TG, int NWN, int FUSE, int NSR = 0, int GATED = 0>
@@ -2610,6 +2693,7 @@ qmm_status launch_tile(GemmArgs& g, hipStream_t s)
         if (hipGetLastError() != hipSuccess) return QMM_ERR_LAUNCH;
         nsr_finalize<<<1, 256, 0, s>>>(g.nsr_partial, total * kWavesM * NWN, g.nsr_out);
     }
+    if constexpr (GATED != 0) { if (g.splits > 1) return launch_gated_reduce<KIND>(g, s); }
     if (g.splits > 1) {
         if (hipGetLastError() != hipSuccess) return QMM_ERR_LAUNCH;
         const int64_t quads = g.M * ((g.N + 3) / 4);
@@ -2772,8 +2856,8 @@ qmm_status launch_gated_few(GemmArgs& g, hipStream_t s)
     g.tiles_m = (int)blocks;
     auto run = [&](auto tb, auto w) {
         constexpr int LDS_BYTES = w.value * tb.value * 2 * 64 * 16;
-        gated_few_kernel<KIND, FA, FB, tb.value, w.value><<<(unsigned)total, 64 * w.value, LDS_BYTES, s>>>(g);
-        return launch_status();
+        gated_few_kernel<KIND, FA, FB, tb.value, w.value><<<dim3((unsigned)total, (unsigned)g.splits), 64 * w.value, LDS_BYTES, s>>>(g);
+        return g.splits > 1 ? launch_gated_reduce<KIND>(g, s) : launch_status();
     };
     using W8 = std::integral_constant<int, 8>;
     if (g.N <= 16) return run(std::integral_constant<int, 1>{}, W8{});
@@ -2785,9 +2869,10 @@ qmm_status launch_gated_few(GemmArgs& g, hipStream_t s)
 template <int KIND, int FA, int FB>
 qmm_status launch_gated(GemmArgs& g, hipStream_t s)
 {
-    if (g.N <= 64) return launch_gated_few<KIND, FA, FB>(g, s);
+    if (g.N <= kGatedFew) return launch_gated_few<KIND, FA, FB>(g, s);
     // Several whole tiles per CU, 16384 x 4096 x 1024 with (g | u), gemm_kernel / gemm_stream_kernel: E4M3 181 / 165 us, bfloat16 270 / 262.  Not for INT8, whose
     // epilogue has no registers left beside the stream's (spilled, 190 against 187).
+    if (g.splits > 1) return launch_tile<KIND, FA, FB, 2, 1, 2, 0, 0, 1>(g, s);
     if constexpr (KIND != KIND_I8) {
         if (use_stream(g, 0) && g.F <= kGatedColumns) return launch_stream<KIND, FA, FB, 1>(g, s);
     }
@@ -2985,7 +3070,9 @@ extern "C" qmm_status qmm_gemm_nsr(const qmm_operand* a, const qmm_operand* b, i
 
 extern "C" size_t qmm_gemm_gated_workspace_size(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K)
 {
-    return 0;
+    if (!a || !b || batch <= 0 || M <= 0 || F <= 0 || K <= 0) return 0;
+    const int splits = plan_gated_splits(M, F, K * (a->format == QMM_FMT_BF16 ? 2 : 1), batch);
+    return splits > 1 ? (size_t)splits * (size_t)batch * (size_t)M * (size_t)F * 8u : 0;
 }
 
 extern "C" qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K,
@@ -3020,7 +3107,12 @@ extern "C" qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b,
     g.db_inner = a->gran.batch_inner > 0 ? a->gran.batch_inner : 1;
     g.da_per_channel = b->gran.per_channel; g.db_per_channel = a->gran.per_channel;
     g.y = h; g.gu = gu; g.y_bf16 = out_dtype == QMM_DT_BF16; g.act = act;
-    g.splits = 1;
+    g.splits = plan_gated_splits(M, F, g.rowbytes, batch);
+    if (g.splits > 1) {
+        if (!workspace || workspace_bytes < (size_t)g.splits * (size_t)batch * (size_t)M * (size_t)F * 8u) return QMM_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return QMM_ERR_ALIGN;
+        g.partial = workspace;
+    }
     return launch_formats(b->format, a->format, g, as_stream(stream), 0);
 }
 #endif  // QMM_GEMM_HAS(0)

@@ -1,4 +1,5 @@
-// The binding's short path: quantized_operand / scale_quantize, gemm and metric of qmm.py for plain tensors, as one native call
+// The binding's short path: quantized_operand / scale_quantize, gemm, metric and the operators around a feed-forward block of qmm.py
+// for plain tensors, as one native call
 // each -- descriptors, outputs and workspace from torch's allocator, the size query and the call on the current stream.  What a
 // small product takes is the host's time: as ctypes calls the four calls of one linear layer took 27 us around 12 us of
 // launches.  Every function returns None where its arguments are not the plain case (tensor subclasses, another device or
@@ -225,6 +226,178 @@ PyObject* metric(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- around a feed-forward block
+// A tensor that kernels on the current device's stream may use.
+bool here(const at::Tensor& x) { return x.is_cuda() && x.layout() == at::kStrided && x.get_device() == c10::hip::current_device(); }
+// None or a plain tensor here; false: neither.
+bool optional(PyObject* o, const at::Tensor** x)
+{
+    *x = nullptr;
+    if (o == Py_None) return true;
+    if (!plain(o)) return false;
+    *x = &THPVariable_Unpack(o);
+    return here(**x);
+}
+bool same(const at::Tensor& x, at::IntArrayRef shape, at::ScalarType type) { return x.sizes() == shape && x.scalar_type() == type; }
+bool weight_of(const at::Tensor* w, int64_t cols, const void** p, int32_t* type)
+{
+    *p = nullptr; *type = QMM_DT_F32;
+    if (!w) return true;
+    if (w->dim() != 1 || w->size(0) != cols || !w->is_contiguous() || !dtype_of(*w, type)) return false;
+    *p = w->data_ptr();
+    return true;
+}
+bool rounding_of(PyObject* mode, PyObject* seed, PyObject* offset, int64_t* m, uint64_t* s, uint64_t* o)
+{
+    if (!number(mode, m) || *m < 0 || *m > 1 || !PyLong_Check(seed) || !PyLong_Check(offset)) return false;
+    *s = PyLong_AsUnsignedLongLongMask(seed); *o = PyLong_AsUnsignedLongLongMask(offset);
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return true;
+}
+// A tuple of tensors, None where there is none.
+PyObject* pack(std::initializer_list<at::Tensor*> tensors)
+{
+    PyObject* r = PyTuple_New((Py_ssize_t)tensors.size());
+    if (!r) return nullptr;
+    Py_ssize_t i = 0;
+    for (at::Tensor* t : tensors) {
+        PyObject* o = t->defined() ? THPVariable_Wrap(std::move(*t)) : (Py_INCREF(Py_None), Py_None);
+        if (!o) { Py_DECREF(r); return nullptr; }
+        PyTuple_SET_ITEM(r, i++, o);
+    }
+    return r;
+}
+void* pointer(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// args: x, weight, fmt, residual, eps, mode, seed, offset, want_y, want_rstd, h_out -> (codes, delta, h, y, rstd)
+PyObject* rmsnorm_quantize(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *w, *r, *given;
+    int64_t fmt, mode; uint64_t seed, offset;
+    if (n != 11 || modes_active() || !plain(args[0]) || !optional(args[1], &w) || !number(args[2], &fmt) || !optional(args[3], &r) ||
+        !PyFloat_Check(args[4]) || !rounding_of(args[5], args[6], args[7], &mode, &seed, &offset) || !PyBool_Check(args[8]) || !PyBool_Check(args[9]) ||
+        !optional(args[10], &given) || fmt < 0 || fmt > 3) Py_RETURN_NONE;
+    const at::Tensor& x = THPVariable_Unpack(args[0]);
+    qmm_tensor t, tr;
+    const void* wp; int32_t wt;
+    if (!here(x) || !describe(x, 1, &t) || !weight_of(w, t.cols, &wp, &wt) || (r && (!same(*r, x.sizes(), x.scalar_type()) || !describe(*r, 1, &tr))) ||
+        (given && (!r || !same(*given, x.sizes(), x.scalar_type()) || !given->is_contiguous()))) Py_RETURN_NONE;
+    at::Tensor codes, delta, h, y, rstd;
+    qmm_status st;
+    {
+        Unlocked unlocked;
+        const at::ScalarType type = x.scalar_type();
+        codes = empty({t.batch, t.rows, t.cols}, at::kByte, x);
+        delta = empty({t.batch * t.rows}, at::kFloat, x);
+        h = given ? *given : r ? empty(x.sizes(), type, x) : x;
+        if (args[8] == Py_True) y = empty(x.sizes(), type, x);
+        if (args[9] == Py_True) rstd = empty({t.batch * t.rows}, at::kFloat, x);
+        st = qmm_rmsnorm_quantize(&t, r ? &tr : nullptr, wp, (qmm_dtype)wt, (float)PyFloat_AS_DOUBLE(args[4]), (qmm_format)fmt, (qmm_round)mode, seed, offset,
+                                  r ? h.data_ptr() : nullptr, pointer(y), static_cast<float*>(pointer(rstd)), static_cast<float*>(delta.data_ptr()),
+                                  static_cast<uint8_t*>(codes.data_ptr()), stream());
+    }
+    if (st != QMM_OK) return PyLong_FromLong(st);
+    return pack({&codes, &delta, &h, &y, &rstd});
+    END_HANDLE_TH_ERRORS
+}
+
+// args: dy, h, rstd, weight, dresidual, want_dw, dx_out -> (dx, dw)
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *w, *r, *given;
+    if (n != 7 || modes_active() || !plain(args[0]) || !plain(args[1]) || !plain(args[2]) || !optional(args[3], &w) || !optional(args[4], &r) ||
+        !PyBool_Check(args[5]) || !optional(args[6], &given)) Py_RETURN_NONE;
+    const at::Tensor &dy = THPVariable_Unpack(args[0]), &h = THPVariable_Unpack(args[1]), &rstd = THPVariable_Unpack(args[2]);
+    const at::ScalarType type = dy.scalar_type();
+    qmm_tensor t, th, tr;
+    const void* wp; int32_t wt;
+    if (!here(dy) || !here(h) || !here(rstd) || !describe(dy, 1, &t) || !same(h, dy.sizes(), type) || !describe(h, 1, &th) ||
+        (r && (!same(*r, dy.sizes(), type) || !describe(*r, 1, &tr))) || rstd.scalar_type() != at::kFloat || !rstd.is_contiguous() ||
+        rstd.numel() != t.batch * t.rows || !weight_of(w, t.cols, &wp, &wt) || (given && (!same(*given, dy.sizes(), type) || !given->is_contiguous())))
+        Py_RETURN_NONE;
+    at::Tensor dx, dw, ws;
+    qmm_status st;
+    {
+        Unlocked unlocked;
+        dx = given ? *given : empty(dy.sizes(), type, dy);
+        size_t bytes = 0;
+        if (args[5] == Py_True) {
+            dw = empty({t.cols}, at::kFloat, dy);
+            bytes = qmm_rmsnorm_backward_workspace_size(&t);
+            if (bytes) ws = empty({(int64_t)bytes}, at::kByte, dy);
+        }
+        st = qmm_rmsnorm_backward(&t, &th, static_cast<const float*>(rstd.data_ptr()), wp, (qmm_dtype)wt, r ? &tr : nullptr, dx.data_ptr(),
+                                  static_cast<float*>(pointer(dw)), pointer(ws), bytes, stream());
+    }
+    if (st != QMM_OK) return PyLong_FromLong(st);
+    return pack({&dx, &dw});
+    END_HANDLE_TH_ERRORS
+}
+
+// args: a, b, activation, out_dtype, want_gu -> (h, gu)
+PyObject* gemm_gated(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *ta, *tb;
+    qmm_operand oa, ob;
+    int64_t act;
+    if (n != 5 || !operand_type || modes_active() || !operand_of(args[0], &ta, &oa) || !operand_of(args[1], &tb, &ob) || !number(args[2], &act) || act < 0 ||
+        act > 1 || !THPDtype_Check(args[3]) || !PyBool_Check(args[4])) Py_RETURN_NONE;
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(args[3])->scalar_type;
+    const int64_t d = ta->dim();
+    if (!here(*ta) || !here(*tb) || (d != 2 && d != 3) || tb->dim() != d || (type != at::kBFloat16 && type != at::kFloat)) Py_RETURN_NONE;
+    const int64_t batch = d == 3 ? ta->size(0) : 1, M = ta->size(d - 2), K = ta->size(d - 1), F = tb->size(d - 2) / 2;
+    if ((d == 3 && tb->size(0) != batch) || tb->size(d - 1) != K || tb->size(d - 2) % 2) Py_RETURN_NONE;
+    at::Tensor h, gu, ws;
+    qmm_status st;
+    {
+        Unlocked unlocked;
+        h = empty({batch, M, F}, type, *ta);
+        if (args[4] == Py_True) gu = empty({batch, M, 2 * F}, type, *ta);
+        const size_t bytes = qmm_gemm_gated_workspace_size(&oa, &ob, batch, M, F, K);
+        if (bytes) ws = empty({(int64_t)bytes}, at::kByte, *ta);
+        st = qmm_gemm_gated(&oa, &ob, batch, M, F, K, (qmm_activation)act, h.data_ptr(), pointer(gu), type == at::kBFloat16 ? QMM_DT_BF16 : QMM_DT_F32,
+                            pointer(ws), bytes, stream());
+    }
+    if (st != QMM_OK) return PyLong_FromLong(st);
+    return pack({&h, &gu});
+    END_HANDLE_TH_ERRORS
+}
+
+// args: dh, gu, activation, fmt, mode, seed, offset, want_codes, want_dgu, dgu_out -> (codes, delta, dgu)
+PyObject* gated_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor* given;
+    int64_t act, fmt, mode; uint64_t seed, offset;
+    if (n != 10 || modes_active() || !plain(args[0]) || !plain(args[1]) || !number(args[2], &act) || !number(args[3], &fmt) || act < 0 || act > 1 || fmt < 0 ||
+        fmt > 3 || !rounding_of(args[4], args[5], args[6], &mode, &seed, &offset) || !PyBool_Check(args[7]) || !PyBool_Check(args[8]) ||
+        !optional(args[9], &given) || (args[7] == Py_False && args[8] == Py_False && !given)) Py_RETURN_NONE;
+    const at::Tensor &dh = THPVariable_Unpack(args[0]), &gu = THPVariable_Unpack(args[1]);
+    qmm_tensor t, tg;
+    if (!here(dh) || !here(gu) || dh.scalar_type() != gu.scalar_type() || dh.dim() != gu.dim() || !describe(dh, 1, &t) || !describe(gu, 1, &tg) ||
+        tg.batch != t.batch || tg.rows != t.rows || tg.cols != 2 * t.cols || (given && (!same(*given, gu.sizes(), gu.scalar_type()) || !given->is_contiguous())))
+        Py_RETURN_NONE;
+    at::Tensor codes, delta, dgu;
+    qmm_status st;
+    {
+        Unlocked unlocked;
+        if (args[7] == Py_True) {
+            codes = empty({t.batch, t.rows, 2 * t.cols}, at::kByte, dh);
+            delta = empty({t.batch * t.rows}, at::kFloat, dh);
+        }
+        if (given) dgu = *given;
+        else if (args[8] == Py_True) dgu = empty(gu.sizes(), gu.scalar_type(), gu);
+        st = qmm_gated_backward(&t, &tg, (qmm_activation)act, (qmm_format)fmt, (qmm_round)mode, seed, offset, pointer(dgu), static_cast<float*>(pointer(delta)),
+                                static_cast<uint8_t*>(pointer(codes)), stream());
+    }
+    if (st != QMM_OK) return PyLong_FromLong(st);
+    return pack({&codes, &delta, &dgu});
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* setup(PyObject*, PyObject* type)
 {
     if (!PyType_Check(type)) { PyErr_SetString(PyExc_TypeError, "a type"); return nullptr; }
@@ -239,6 +412,10 @@ PyMethodDef methods[] = {
     {"quantized_operand", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantized_operand)), METH_FASTCALL, nullptr},
     {"gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gemm)), METH_FASTCALL, nullptr},
     {"metric", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(metric)), METH_FASTCALL, nullptr},
+    {"rmsnorm_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rmsnorm_quantize)), METH_FASTCALL, nullptr},
+    {"rmsnorm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rmsnorm_backward)), METH_FASTCALL, nullptr},
+    {"gemm_gated", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gemm_gated)), METH_FASTCALL, nullptr},
+    {"gated_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gated_backward)), METH_FASTCALL, nullptr},
     {"setup", setup, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_qmm_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,7 +1,7 @@
 """Thin binding of libqmm.so (include/qmm.h).  Argument marshalling only: every step of the path runs in the HIP kernels.
-torch is used for device memory and the current stream.  All calls go through ctypes; quantized_operand, scale_quantize, gemm
-and metric first try the native short path for plain tensors (csrc/qmm_host.cpp), which does the same with a fifth of the
-host time.  There is no CPU fallback: a missing or unloadable library raises."""
+torch is used for device memory and the current stream.  All calls go through ctypes; quantized_operand, scale_quantize, gemm,
+metric and the operators around a feed-forward block first try the native short path for plain tensors (csrc/qmm_host.cpp), which does
+the same with a fifth of the host time.  There is no CPU fallback: a missing or unloadable library raises."""
 import collections
 import ctypes
 import importlib.util
@@ -54,7 +54,7 @@ class _NoShortPath:
     @staticmethod
     def _decline(*_):
         return None
-    scale_quantize = quantized_operand = gemm = metric = _decline
+    scale_quantize = quantized_operand = gemm = metric = rmsnorm_quantize = rmsnorm_backward = gemm_gated = gated_backward = _decline
 
 
 def _host():
@@ -430,6 +430,11 @@ def rmsnorm_quantize(x, weight, fmt, residual=None, eps=1e-6, mode=RTNE, seed=0,
     """qmm_rmsnorm_quantize on [rows, cols] or [batch, rows, cols]: Normed(codes [batch, rows, cols], delta, h, y, rstd).  codes and delta are an
     operand with per_channel=True and batch_groups=batch; h is x + residual (x without one), y and rstd are None unless wanted.
     `h_out`: where h goes, e.g. the residual itself."""
+    r = (_short or _host()).rmsnorm_quantize(x, weight, fmt, residual, eps, mode, seed, offset, want_y, want_rstd, h_out)
+    if type(r) is int:
+        _check(r, "qmm_rmsnorm_quantize")
+    if r is not None:
+        return Normed._make(r)
     L = lib()
     dev = _on(x.device, x, weight, residual, h_out)
     t = _row_desc(x)
@@ -452,6 +457,11 @@ def rmsnorm_quantize(x, weight, fmt, residual=None, eps=1e-6, mode=RTNE, seed=0,
 
 def rmsnorm_backward(dy, h, rstd, weight, dresidual=None, want_dw=True, dx_out=None):
     """qmm_rmsnorm_backward: (dx, dw); dw is float32, or None unless wanted.  `dx_out`: where dx goes, e.g. dy itself."""
+    r = (_short or _host()).rmsnorm_backward(dy, h, rstd, weight, dresidual, want_dw, dx_out)
+    if type(r) is int:
+        _check(r, "qmm_rmsnorm_backward")
+    if r is not None:
+        return r
     L = lib()
     dev = _on(dy.device, dy, h, rstd, weight, dresidual, dx_out)
     t, th = _row_desc(dy), _row_desc(h, dy.shape, dy.dtype)
@@ -469,6 +479,11 @@ def rmsnorm_backward(dy, h, rstd, weight, dresidual=None, want_dw=True, dx_out=N
 def gemm_gated(a, b, activation=SILU, out_dtype=torch.bfloat16, want_gu=False):
     """qmm_gemm_gated on two (data, Operand) pairs as `gemm` takes them, b = ([batch, 2 F, K], Operand) with the gate's rows first:
     h [batch, M, F], or (h, gu [batch, M, 2 F]) when want_gu."""
+    r = (_short or _host()).gemm_gated(a, b, activation, out_dtype, want_gu)
+    if type(r) is int:
+        _check(r, "qmm_gemm_gated")
+    if r is not None:
+        return r if want_gu else r[0]
     L = lib()
     (ta, oa), (tb, ob) = a, b
     dev = _on(ta.device, ta, tb)
@@ -490,6 +505,11 @@ def gemm_gated(a, b, activation=SILU, out_dtype=torch.bfloat16, want_gu=False):
 def gated_backward(dh, gu, activation=SILU, fmt=E5M2, mode=RTNE, seed=0, offset=0, want_codes=True, want_dgu=False, dgu_out=None):
     """qmm_gated_backward on dh [.., F] and gu [.., 2 F]: GatedGradient(codes [batch, rows, 2 F], delta, dgu), None for what is not wanted.
     codes and delta are an operand with per_channel=True and batch_groups=batch.  `dgu_out`: where dgu goes, e.g. gu itself."""
+    r = (_short or _host()).gated_backward(dh, gu, activation, fmt, mode, seed, offset, want_codes, want_dgu, dgu_out)
+    if type(r) is int:
+        _check(r, "qmm_gated_backward")
+    if r is not None:
+        return GatedGradient._make(r)
     L = lib()
     dev = _on(dh.device, dh, gu, dgu_out)
     t, tg = _row_desc(dh), _row_desc(gu, (*dh.shape[:-1], 2 * dh.shape[-1]), dh.dtype)

@@ -100,6 +100,11 @@ def test_gated_refusals(L):
     for n in ((0, 8, 16, 32), (1, 0, 16, 32), (1, 8, 0, 32)):
         assert run(O(data=None), O(), n=n, h=None) == 0 and L.qmm_gemm_gated_workspace_size(ref(O()), ref(O()), *n) == 0
     assert L.qmm_gemm_gated_workspace_size(None, ref(O()), 1, 8, 16, 32) == 0
+    # few columns and a long contraction: split, with a workspace for the parts
+    for n in ((1, 8, 64, 8192), (1, 200, 100, 4096), (2, 64, 16, 6144)):
+        need = L.qmm_gemm_gated_workspace_size(ref(O()), ref(O()), *n)
+        assert need > 0 and need % (8 * n[0] * n[1] * n[2]) == 0
+        assert run(O(), O(), n=n) == 6 and run(O(), O(), n=n, ws=p, nws=need - 1) == 6 and run(O(), O(), n=n, ws=ctypes.c_void_p(0x10004), nws=need) == 4
 
     T = lambda **k: qmm.Tensor(*{**dict(data=0x20000, dtype=qmm.DT_F32, axis=1, b=2, r=4, c=16, bs=128, rs=32), **k}.values())
 

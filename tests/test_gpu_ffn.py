@@ -213,7 +213,8 @@ def gated_reference(a, b, da, db, kind, fmt, fmt_b=None):
 
 
 GATED = [(1, 1, 16), (1, 33, 64), (1, 512, 2048), (2, 100, 4096), (5, 64, 272), (16, 256, 1024), (17, 130, 144), (24, 500, 784), (33, 96, 400), (64, 64, 128),
-         (65, 63, 128), (100, 200, 304), (129, 129, 144), (130, 257, 1040), (256, 128, 512), (300, 640, 384), (512, 256, 256), (1031, 100, 784), (1024, 1024, 96)]
+         (65, 63, 128), (100, 200, 304), (129, 129, 144), (130, 257, 1040), (256, 128, 512), (300, 640, 384), (512, 256, 256), (1031, 100, 784), (1024, 1024, 96),
+         (1, 64, 8192), (3, 1000, 6160), (20, 70, 6144), (64, 130, 7000 // 16 * 16), (40, 2000, 6160), (70, 61, 4096), (200, 130, 2064), (129, 512, 4080)]
 
 
 @pytest.mark.parametrize("fa,fb", [(qmm.INT8, qmm.INT8), (qmm.E4M3, qmm.E4M3), (qmm.E4M3, qmm.E5M2), (qmm.E5M2, qmm.E4M3), (qmm.E5M2, qmm.E5M2), (qmm.BF16, qmm.BF16)])
@@ -238,7 +239,7 @@ def test_gated_product(m, f, k, fa, fb):
 
 
 @pytest.mark.parametrize("fmt", [qmm.INT8, qmm.E4M3, qmm.BF16])
-@pytest.mark.parametrize("batch,m,f,k", [(3, 1, 40, 96), (5, 20, 64, 128), (2, 150, 130, 272), (3, 300, 200, 128)])
+@pytest.mark.parametrize("batch,m,f,k", [(3, 1, 40, 96), (5, 20, 64, 128), (2, 150, 130, 272), (3, 300, 200, 128), (3, 7, 50, 6400), (2, 130, 70, 4096)])
 def test_gated_product_in_batches(batch, m, f, k, fmt):
     a, va, da = coded(normal(1, batch, m, k), fmt)
     b, vb, db = coded(normal(2, batch, 2 * f, k, scale=1.5 / k ** 0.5), fmt)
@@ -394,6 +395,33 @@ def test_gated_backward_special_rows():
 
 
 # ------------------------------------------------------------------------------------------------ together
+def test_native_calls_equal_the_ctypes_ones(monkeypatch):
+    x, r, w = normal(1, 2, 30, 100, dtype=BF).to(DEV), normal(2, 2, 30, 100, dtype=BF).to(DEV), normal(3, 100).to(DEV)
+    dh, gu = normal(4, 30, 40).to(DEV), normal(5, 30, 80).to(DEV)
+    (ca, oa), _ = qmm.quantized_operand(normal(6, 30, 96).to(DEV), 1, qmm.E4M3, per_channel=True)
+    (cb, ob), _ = qmm.quantized_operand(normal(7, 80, 96).to(DEV), 1, qmm.E4M3, per_channel=True)
+
+    def every():
+        a = qmm.rmsnorm_quantize(x, w, qmm.E4M3, residual=r, mode=qmm.STOCHASTIC, seed=2 ** 64 - 1, offset=3, want_y=True, want_rstd=True)
+        b = qmm.rmsnorm_quantize(x, None, qmm.INT8, eps=1)
+        c = qmm.rmsnorm_backward(x, a.h, a.rstd, w, dresidual=r)
+        d = qmm.rmsnorm_backward(x, a.h, a.rstd, None, want_dw=False)
+        e = qmm.gemm_gated((ca, oa), (cb, ob), qmm.GELU, F32, want_gu=True)
+        f = qmm.gemm_gated((ca, oa), (cb, ob))
+        g = qmm.gated_backward(dh, gu, qmm.GELU, qmm.INT8, want_dgu=True)
+        h = qmm.gated_backward(dh, gu, want_codes=False, dgu_out=gu.clone())
+        return [*a, *b, *c, *d, *e, f, *g, *h]
+    native = every()
+    monkeypatch.setattr(qmm, "_short", qmm._NoShortPath)
+    for p, q in zip(native, every(), strict=True):
+        assert (p is None and q is None) or R.same_bits(p, q)
+    for call in (lambda: qmm.rmsnorm_quantize(x, w, qmm.E4M3, eps=-1.0), lambda: qmm.gemm_gated((ca, oa), (cb, ob), 5), lambda: qmm.gated_backward(dh, gu, fmt=qmm.BF16)):
+        for short in (qmm._NoShortPath, None):
+            monkeypatch.setattr(qmm, "_short", short)
+            with pytest.raises(qmm.QmmError):
+                call()
+
+
 def block(x, stream, p, dout):
     """A gated feed-forward block behind its norm, forward and backward, as a training step runs it: 8-bit products, upstream gradients in E5M2."""
     q = lambda t, fmt, axis=1: qmm.quantized_operand(t, axis, fmt, per_channel=True)[0]
