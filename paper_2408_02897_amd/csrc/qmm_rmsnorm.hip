@@ -27,6 +27,7 @@ struct NormArgs {
     int64_t batch, rows, cols;
     uint64_t seed, offset;
     float qmax; int fmt;
+    int streaming;                             // h and y go past the caches (host)
 };
 
 // 1 / sqrt(mean + eps), both operations correctly rounded
@@ -66,7 +67,8 @@ rmsnorm_rows(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = Vec<T>::at(w[k], e) + Vec<T>::at(q[k], e);
                 w[k] = pack_row<T>(v);
-                store_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
+                if (a.streaming) stream_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
+                else store_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
             }
         }
         float y[NV][V], sum = 0.0f;
@@ -98,7 +100,10 @@ rmsnorm_rows(NormArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) y[k][e] *= rstd;
             const int64_t p = id * a.cols + c;
-            if (a.y) store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
+            if (a.y) {
+                if (a.streaming) stream_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
+                else store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
+            }
             store_codes<T>(a.codes + p, encode_values<V, MODE>(y[k], rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
         }
     }
@@ -174,52 +179,67 @@ struct NormGradArgs {
     int64_t shares;                                    // of them
 };
 
+// A thread's next row is on its way while it works on the current one; workgroups of 1024 threads, whose threads have 128 registers, do without,
+// and fetch the weights anew for every row.
 template <typename T, int LPR, int NV> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
 rmsnorm_grad_rows(NormGradArgs a)
 {
     constexpr int V = Vec<T>::V, THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
+    constexpr bool AHEAD = LPR < 1024;
     __shared__ typename RowReduce<LPR>::Shared sh;
     __shared__ float s_dw[RPB > 1 ? RPB : 1][RPB > 1 ? LPR * NV * V : 1];
     const int64_t total = a.batch * a.rows;
     const int c0 = (int)(threadIdx.x % LPR) * V;
     float weight[NV][V], dw[NV][V];
+    auto load_weights = [&]() {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, (int)a.cols - c0 - k * LPR * V, weight[k]);
+        for (int k = 0; k < NV; ++k) load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, (int)a.cols - c0 - k * LPR * V, weight[k]);
+    };
+    if constexpr (AHEAD) load_weights();
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[k][e] = 0.0f;
-    }
-    int turn = 0;
-    for (int64_t blk = blockIdx.x; blk * RPB < total; blk += gridDim.x, turn ^= 1) {
+    struct Row { u32x4 g[NV], w[NV], q[NV]; float rstd; };      // dy, h, dresidual
+    auto fetch = [&](int64_t blk, Row& r) {
         const int64_t id = blk * RPB + threadIdx.x / LPR;
         const bool live = id < total;
         const int64_t b = live && a.batch > 1 ? id / a.rows : 0, i = live ? id - b * a.rows : 0;
         const int cols = live ? (int)a.cols : 0;
         const T* dy = static_cast<const T*>(a.dy) + b * a.dy_batch + i * a.dy_row;
         const T* h = static_cast<const T*>(a.h) + b * a.h_batch + i * a.h_row;
-        u32x4 g[NV], w[NV], q[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * LPR * V;
-            g[k] = load_row<T>(dy + c, cols - c);
-            w[k] = load_row<T>(h + c, cols - c);
-            q[k] = u32x4{0u, 0u, 0u, 0u};
-            if (a.r) q[k] = load_row<T>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row + c, cols - c);
+            r.g[k] = load_row<T>(dy + c, cols - c);
+            r.w[k] = load_row<T>(h + c, cols - c);
+            r.q[k] = u32x4{0u, 0u, 0u, 0u};
+            if (a.r) r.q[k] = load_row<T>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row + c, cols - c);
         }
-        const float rstd = live ? a.rstd[id] : 0.0f;
+        r.rstd = live ? a.rstd[id] : 0.0f;
+    };
+    Row row;
+    if (AHEAD && (int64_t)blockIdx.x * RPB < total) fetch(blockIdx.x, row);
+    int turn = 0;
+    for (int64_t blk = blockIdx.x; blk * RPB < total; blk += gridDim.x, turn ^= 1) {
+        const int64_t id = blk * RPB + threadIdx.x / LPR;
+        const int cols = id < total ? (int)a.cols : 0;
+        Row next;
+        if constexpr (AHEAD) { if ((blk + gridDim.x) * RPB < total) fetch(blk + gridDim.x, next); }
+        else { fetch(blk, row); load_weights(); }
+        const float rstd = row.rstd;
         float sum = 0.0f;
         uint32_t none = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = Vec<T>::at(g[k], e), n = Vec<T>::at(w[k], e) * rstd;
+                const float d = Vec<T>::at(row.g[k], e), n = Vec<T>::at(row.w[k], e) * rstd;
                 sum = fmaf(d * weight[k][e], n, sum);
                 dw[k][e] = fmaf(d, n, dw[k][e]);
             }
         RowReduce<LPR>::run(sum, none, sh, turn);
         const float mean = sum / (float)a.cols;
-        if (!live) continue;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * LPR * V, left = cols - c;
@@ -227,11 +247,12 @@ rmsnorm_grad_rows(NormGradArgs a)
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float n = Vec<T>::at(w[k], e) * rstd;
-                v[e] = fmaf(rstd, fmaf(-n, mean, Vec<T>::at(g[k], e) * weight[k][e]), Vec<T>::at(q[k], e));
+                const float n = Vec<T>::at(row.w[k], e) * rstd;
+                v[e] = fmaf(rstd, fmaf(-n, mean, Vec<T>::at(row.g[k], e) * weight[k][e]), Vec<T>::at(row.q[k], e));
             }
             store_row<T>(static_cast<T*>(a.dx) + id * a.cols + c, pack_row<T>(v), left);
         }
+        if constexpr (AHEAD) row = next;
     }
     if (!a.partial) return;
     if constexpr (RPB > 1) {
@@ -321,37 +342,49 @@ rmsnorm_grad_columns(NormGradArgs a)                   // grid (columns, shares)
         store_row<float>(a.partial + (int64_t)blockIdx.y * a.cols + c + 4 * q, pack_row<float>(dw + 4 * q), left - 4 * q);
 }
 
-// dw = the sum of the shares: a workgroup takes 64 columns, its wavefronts every sixteenth share each, in order.
+// dw = the sum of the shares, in an order fixed by their number: a workgroup takes 16 columns, sixty-four lanes a column every sixty-fourth share each.
+// (64 columns and sixteen lanes a column, a quarter of the workgroups: 512 shares of 1000 columns 3.9 us, of 4096 4.8.)
 __global__ void __launch_bounds__(1024)
 rmsnorm_grad_fold(NormGradArgs a)
 {
-    __shared__ float part[16][kWave];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+    constexpr int C = 16, L = 1024 / C;
+    __shared__ float part[L][C + 1];
+    const int c_in = threadIdx.x % C, l = threadIdx.x / C;
+    const int64_t c = (int64_t)blockIdx.x * C + c_in;
     float s = 0.0f;
     if (c < a.cols) {
 #pragma unroll 8
-        for (int64_t p = wave; p < a.shares; p += 16) s += a.partial[p * a.cols + c];
+        for (int64_t p = l; p < a.shares; p += L) s += a.partial[p * a.cols + c];
     }
-    part[wave][lane] = s;
+    part[l][c_in] = s;
     __syncthreads();
-    if (wave == 0 && c < a.cols) {
+    if (threadIdx.x < kWave) {                               // four lanes a column
+        const int k = threadIdx.x % C, first = threadIdx.x / C * (L / 4);
         s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) s += part[k][lane];
-        a.dw[c] = s;
+        for (int i = 0; i < L / 4; ++i) s += part[first + i][k];
+        s += __shfl_xor(s, 16, kWave);
+        s += __shfl_xor(s, 32, kWave);
+        const int64_t f = (int64_t)blockIdx.x * C + k;
+        if (threadIdx.x < C && f < a.cols) a.dw[f] = s;
     }
 }
 
-// Shares of dw: workgroups that go over rows, of columns' parts of rows where rows are long.
+// Shares of dw: workgroups that go over rows, of columns' parts of rows where rows are long.  Two workgroups a CU, one of 1024 threads: enough to keep
+// the rows coming, and every further one is a share more to write and fold (bfloat16 16384 x 4096, 256 / 384 / 512 / 768 / 1024 workgroups 135 / 109 / 104 / 108 /
+// 119 us; binary32 1000 x 12000, 1024 threads, 256 / 512: 53 / 61).
 int64_t shares_of(const qmm_tensor* t)
 {
     const int64_t total = t->batch * t->rows;
     if (t->cols > kRowElements) return std::min<int64_t>(total, 64);
-    int64_t blocks = 0;
-    auto count = [&](auto lpr, auto) { constexpr int rpb = lpr.value < 256 ? 256 / lpr.value : 1; blocks = (total + rpb - 1) / rpb; };
+    int64_t blocks = 0, most = 512;
+    auto count = [&](auto lpr, auto) {
+        constexpr int rpb = lpr.value < 256 ? 256 / lpr.value : 1;
+        blocks = (total + rpb - 1) / rpb;
+        if (lpr.value == 1024) most = 256;
+    };
     if (t->dtype == QMM_DT_BF16) for_row_size<uint16_t>(t->cols, count); else for_row_size<float>(t->cols, count);
-    return std::min<int64_t>(blocks, 512);
+    return std::min(blocks, most);
 }
 
 template <typename T, int MODE> qmm_status launch_norm(const NormArgs& a, hipStream_t s)
@@ -382,7 +415,7 @@ template <typename T> qmm_status launch_norm_grad(NormGradArgs& a, hipStream_t s
     }
     if (a.partial) {
         if (hipGetLastError() != hipSuccess) return QMM_ERR_LAUNCH;
-        rmsnorm_grad_fold<<<(unsigned)((a.cols + kWave - 1) / kWave), 1024, 0, s>>>(a);
+        rmsnorm_grad_fold<<<(unsigned)((a.cols + 15) / 16), 1024, 0, s>>>(a);
     }
     return launch_status();
 }
@@ -426,6 +459,10 @@ extern "C" qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor
     a.batch = x->batch; a.rows = x->rows; a.cols = x->cols;
     a.seed = seed; a.offset = offset; a.qmax = host_qmax(fmt); a.fmt = fmt;
     if (a.cols == 0) a.r = nullptr;
+    // h is wanted by the next addition to the residual stream, y by the backward pass: from where they would fill the caches between here and there
+    // they go past them, the codes, which the next product reads, do not (bfloat16 16384 x 4096 with y 115 -> 108 us, 8192 x 8192 97 -> 90,
+    // binary32 16384 x 4096 168 -> 154; 16384 x 1024, 33 MB, 22.7 -> 22.2)
+    a.streaming = a.batch * a.rows * a.cols * (x->dtype == QMM_DT_BF16 ? 2 : 4) >= (int64_t)64 << 20;
     hipStream_t s = as_stream(stream);
     if (x->dtype == QMM_DT_BF16)
         return mode == QMM_ROUND_RTNE ? launch_norm<uint16_t, QMM_ROUND_RTNE>(a, s) : launch_norm<uint16_t, QMM_ROUND_STOCHASTIC>(a, s);
@@ -471,7 +508,7 @@ extern "C" qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tenso
     a.dw = dw_out;
     hipStream_t s = as_stream(stream);
     if (empty) {                                             // no rows: dw is a sum of none
-        if (dw_out) rmsnorm_grad_fold<<<(unsigned)((a.cols + kWave - 1) / kWave), 1024, 0, s>>>(a);
+        if (dw_out) rmsnorm_grad_fold<<<(unsigned)((a.cols + 15) / 16), 1024, 0, s>>>(a);
         return launch_status();
     }
     a.shares = shares_of(dy);

@@ -38,6 +38,12 @@ template <typename T> QMM_DEV void store_row(T* p, const u32x4& w, int left)
             else p[e] = (T)(w[e >> 1] >> (16 * (e & 1)));
         }
 }
+// The same past the caches, for outputs that are wanted again much later; `p` on a 16-byte boundary, or an ordinary store.
+template <typename T> QMM_DEV void stream_row(T* p, const u32x4& w, int left)
+{
+    if (left >= Vec<T>::V && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+    else store_row<T>(p, w, left);
+}
 // V elements of a vector of either type (the norm's weights), ones where there is none
 template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int left, float (&out)[V])
 {
