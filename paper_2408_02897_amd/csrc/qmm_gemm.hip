@@ -180,6 +180,7 @@ template <int T> QMM_DEV void store_bf16(uint16_t* dst, const float (&v)[T])
     else *reinterpret_cast<u1u*>(dst) = u1u{pk[0]};
 }
 
+constexpr int kGatedSlots = 3;                             // ring of gated_deep_kernel
 constexpr int kGatedFew = 64;                              // tokens up to which gated_few_kernel serves
 constexpr int64_t kGatedColumns = int64_t(1) << 22;          // F up to which 64 rows of (g | u) in binary32 lie within 32-bit offsets
 
@@ -2399,6 +2400,202 @@ gemm_deep_kernel(GemmArgs g)
         }
 }
 
+// A gated product of few tiles, as gemm_deep_kernel is for the plain one: tiles of 32 columns (64 weight rows) x 128 tokens, four wavefronts of
+// 32 tokens each, one barrier a step and a ring of three slabs of both operands (72 KB), all but one on their way.  (Six slabs: no faster where a CU gets
+// one workgroup, 8.6 us against 8.5, and slower where it gets two.)  LDS layout, fragments and order of K are gemm_kernel's: the accumulators are the same bits.
+template <int KIND, int FA, int FB>
+__global__ void __launch_bounds__(256, 1)
+gated_deep_kernel(GemmArgs g)
+{
+    constexpr int SLOTS = kGatedSlots;
+    constexpr bool F8 = (KIND == KIND_F8);
+    constexpr int BM = 64, BN = 128, WN = 32;
+    constexpr int R = F8 ? 16 : 32;
+    constexpr int BLOCKS_M = BM / R, TILES_N = WN / R, NP = BLOCKS_M / 2;
+    constexpr int KS = F8 ? 1 : 4;
+    constexpr int REGS = F8 ? 4 : 16;
+    constexpr int A_SLOT = BM * kSlabBytes, SLOT = A_SLOT + BN * kSlabBytes;   // a slab of the weights, then one of the tokens
+    constexpr int UA = BM / 8 / 4, UB = BN / 8 / 4, UNITS = UA + UB;           // copies of 8 LDS rows per wavefront
+    static_assert(UA % 2 == 0 && UB % 2 == 0, "a wavefront's units start on an even LDS row pair");
+    static_assert(SLOTS == 3, "the waits below");
+    using AccT = typename std::conditional<F8, v4f, typename std::conditional<KIND == KIND_I8, v16i, v16f>::type>::type;
+    using Frag = typename std::conditional<F8, v8i, v4i>::type;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles_per_batch = (uint32_t)g.tiles_m * (uint32_t)g.tiles_n;
+    const int64_t bidx = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / tiles_per_batch));
+    const uint32_t t = blockIdx.x - (uint32_t)bidx * tiles_per_batch;
+    const int64_t tile_m = __builtin_amdgcn_readfirstlane((int)(t / (uint32_t)g.tiles_n));
+    const int64_t tile_n = __builtin_amdgcn_readfirstlane((int)(t % (uint32_t)g.tiles_n));
+    const int64_t f0 = tile_m * (BM / 2), n0 = tile_n * BN;
+    const int rowbytes = (int)g.rowbytes;
+    const int nk = (rowbytes + kSlabBytes - 1) / kSlabBytes;
+    const uint8_t* a_tile = g.a + (bidx * g.M + f0) * g.rowbytes;
+    const uint8_t* b_tile = g.b + (bidx * g.N + n0) * g.rowbytes;
+
+    // copy sources, as in gemm_deep_kernel; a unit of the weights lies in one block, of gate or of up
+    uint32_t src[UNITS];
+    int chunk[UNITS];
+    const uint8_t* base[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        const bool is_a = i < UA;
+        const int unit = is_a ? wave * UA + i : wave * UB + i - UA, p = unit * 8 + (lane >> 3);
+        chunk[i] = (lane & 7) ^ ((p >> 1) & 7);
+        int64_t row;
+        if (is_a) {
+            bool up;
+            row = gated_row<F8, NP>(p, up);
+            row = f0 + row < g.F ? row : g.F - 1 - f0;
+            base[i] = a_tile + (((unit * 8 / R) & 1) != 0 ? g.F * g.rowbytes : 0);
+        } else {
+            row = WN * (p / WN) + TILES_N * (p % R) + (p / R) % TILES_N;
+            row = n0 + row < g.N ? row : g.N - 1 - n0;
+            base[i] = b_tile;
+        }
+        src[i] = (uint32_t)(row * g.rowbytes + chunk[i] * 16);
+    }
+    typedef __attribute__((address_space(3))) uint8_t* lds_ptr_t;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
+    auto copy_slab = [&](int slab, int slot) {
+        const int k0 = slab * kSlabBytes;
+        const bool whole = k0 + kSlabBytes <= rowbytes;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const uint32_t off = slot * SLOT + (i < UA ? (wave * UA + i) * 1024 : A_SLOT + (wave * UB + i - UA) * 1024);
+            // (a chunk past the end of the rows: zeros; every slab counts the same number of copies, masked off or not)
+            if (whole || k0 + chunk[i] * 16 < rowbytes) dma16_uniform(base[i] + k0, src[i], lds_base + off);
+            if (!whole && k0 + chunk[i] * 16 >= rowbytes) *reinterpret_cast<u32x4*>(lds + off + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+
+    AccT acc[BLOCKS_M][TILES_N];
+#pragma unroll
+    for (int i = 0; i < BLOCKS_M; ++i)
+#pragma unroll
+        for (int j = 0; j < TILES_N; ++j)
+#pragma unroll
+            for (int e = 0; e < REGS; ++e) acc[i][j][e] = 0;
+
+    const int frow = lane & (R - 1);
+    const int fkey = (frow >> 1) & 7;
+    const int fsel = F8 ? (lane >> 4) : (lane >> 5);
+    int coff[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) coff[s] = ((F8 ? fsel : 2 * s + fsel) ^ fkey) * 16;
+    auto read_frag = [&](const uint8_t* row_ptr, int s) -> Frag {
+        if constexpr (F8) {
+            const v4i p0 = *reinterpret_cast<const v4i*>(row_ptr + coff[0]);
+            const v4i p1 = *reinterpret_cast<const v4i*>(row_ptr + (coff[0] ^ 64));
+            return v8i{p0[0], p0[1], p0[2], p0[3], p1[0], p1[1], p1[2], p1[3]};
+        } else {
+            return *reinterpret_cast<const v4i*>(row_ptr + coff[s]);
+        }
+    };
+    auto mma = [&](const Frag& fa, const Frag& fb, AccT& c) {
+        if constexpr (F8) {
+            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb, c, FA == QMM_FMT_E5M2 ? 1 : 0,
+                                                                 FB == QMM_FMT_E5M2 ? 1 : 0, 0, 0, 0, 0);
+        } else if constexpr (KIND == KIND_I8) {
+            c = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, c, 0, 0, 0);
+        } else {
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, fa), __builtin_bit_cast(v8bf, fb), c, 0, 0, 0);
+        }
+    };
+
+#pragma unroll
+    for (int s = 0; s < SLOTS - 1; ++s)
+        if (s < nk) copy_slab(s, s);
+    int slot = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        // slab kt has landed: only the copies of the slabs after it (at most SLOTS - 2) may be outstanding
+        const int newer = min(SLOTS - 2, nk - 1 - kt);
+        if (newer == SLOTS - 2) wait_vm_lgkm<(SLOTS - 2) * UNITS>();
+        else wait_vm_lgkm<0>();
+        __syncthreads();
+        const int free_slot = slot == 0 ? SLOTS - 1 : slot - 1;            // read in step kt - 1
+        if (kt + SLOTS - 1 < nk) copy_slab(kt + SLOTS - 1, free_slot);
+        const uint8_t* sa = lds + slot * SLOT + frow * kSlabBytes;
+        const uint8_t* sb = lds + slot * SLOT + A_SLOT + (wave * WN + frow) * kSlabBytes;
+        Frag fa[BLOCKS_M][KS], fb[TILES_N][KS];
+#pragma unroll
+        for (int j = 0; j < TILES_N; ++j)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) fb[j][s] = read_frag(sb + j * R * kSlabBytes, s);
+#pragma unroll
+        for (int i = 0; i < BLOCKS_M; ++i)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) fa[i][s] = read_frag(sa + i * R * kSlabBytes, s);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < BLOCKS_M; ++i)
+#pragma unroll
+                for (int j = 0; j < TILES_N; ++j) mma(fa[i][s], fb[j][s], acc[i][j]);
+        slot = slot == SLOTS - 1 ? 0 : slot + 1;
+    }
+
+    // ---- epilogue: (acc * delta[token]) * delta[column], in that order
+    constexpr bool descale = (KIND != KIND_BF16);
+    const float* da = g.da ? g.da + ((bidx / g.da_inner) % g.da_groups) * (g.da_per_channel ? g.M : 1) : nullptr;
+    const float* db = g.db ? g.db + ((bidx / g.db_inner) % g.db_groups) * (g.db_per_channel ? g.N : 1) : nullptr;
+    const int64_t n_base = n0 + wave * WN, n = n_base + TILES_N * (lane & (R - 1));
+    const int lane_row = F8 ? 4 * (lane >> 4) : 4 * (lane >> 5);
+    auto column = [&](int p, int v, bool& up) -> int64_t { return f0 + gated_row<F8, NP>(2 * p * R + (F8 ? lane_row + v : 8 * (v >> 2) + lane_row + (v & 3)), up); };
+    float st[TILES_N], sw[NP][2][REGS];
+#pragma unroll
+    for (int tt = 0; tt < TILES_N; ++tt) {
+        st[tt] = 1.0f;
+        if constexpr (descale) st[tt] = db[g.db_per_channel ? (n + tt < g.N ? n + tt : g.N - 1) : 0];
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int v = 0; v < REGS; ++v) {
+            bool up;
+            const int64_t f = min(column(p, v, up), g.F - 1);
+            sw[p][0][v] = sw[p][1][v] = 1.0f;
+            if constexpr (descale) {
+                sw[p][0][v] = da[g.da_per_channel ? f : 0];
+                sw[p][1][v] = da[g.da_per_channel ? g.F + f : 0];
+            }
+        }
+    auto value = [&](int p, int half, int v, int tt) -> float {
+        float a;
+        if constexpr (KIND == KIND_I8) a = (float)acc[2 * p + half][tt][v]; else a = acc[2 * p + half][tt][v];
+        if constexpr (descale) a = (a * st[tt]) * sw[p][half][v];
+        return a;
+    };
+    if (f0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0 && g.F <= kGatedColumns) {
+        const int es = g.y_bf16 ? 2 : 4;
+        gated_forms(g, [&](auto act, auto bf, auto kept) {
+#pragma unroll
+            for (int tt = 0; tt < TILES_N; ++tt) {
+                uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.N + n_base + tt) * g.F + f0) * es;
+                uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.N + n_base + tt) * 2 * g.F + f0) * es;
+                gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
+                    h, gu, g.F, lane, [&](int p, int half, int v) { return value(p, half, v, tt); }, []() {});
+            }
+        });
+        return;
+    }
+    auto edge = [&](auto act) {
+#pragma unroll
+        for (int tt = 0; tt < TILES_N; ++tt)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int v = 0; v < REGS; ++v) {
+                    bool up;
+                    const float gv = value(p, 0, v, tt), uv = value(p, 1, v, tt);
+                    gated_one(g, bidx, n + tt, column(p, v, up), activate<decltype(act)::value>(gv) * uv, gv, uv);
+                }
+    };
+    if (g.act == QMM_ACT_SILU) edge(std::integral_constant<int, QMM_ACT_SILU>{}); else edge(std::integral_constant<int, QMM_ACT_GELU>{});
+}
+
 // A gated product of few tokens (at most 64): it takes as long as its weights are on their way from memory, 2 F K codes, so the point is to have
 // many of them on the way at any time.  A workgroup of W wavefronts takes 16 columns -- 16 rows of gate, 16 of up -- and the wavefronts share
 // the contraction, slab by slab in turn, so that together they read whole stretches of a row.  Fragments go straight into registers, up to
@@ -2642,16 +2839,19 @@ int plan_splits(int64_t M, int64_t N, int64_t rowbytes, int64_t batch, int fuse)
     return splits >= 2 ? (int)splits : 1;
 }
 
-// The same for gated products of M tokens: 128 x 128 tiles (64 columns of both halves) as above, or, up to 64 tokens, the workgroups of 16 columns of
-// gated_few_kernel, of which a CU takes two.  The second kernel takes 3 us, so few tokens are split from 48 slabs on (E4M3, one token, unsplit / split: 512 x 8192
-// 11.5 / 7.5 us, 1000 x 2000 5.1 / 7.0; 64 tokens 1024 x 8192 25.5 / 16.8).  Its grid has the tokens and matrices for dimensions.
+// The same for gated products of M tokens: up to 64 of them the workgroups of 16 columns of gated_few_kernel, of which a CU takes two; else 128 x 128
+// tiles (64 columns of both halves), one a CU.  The second kernel takes 3 to 4 us and more where the parts are large, an unsplit product 0.6 us a slab: split
+// from 48 slabs on, or 24 where at most 32 tiles would work (E4M3, unsplit / split: one token 512 x 8192 11.5 / 7.5 us, 1000 x 2000 5.1 / 7.0,
+// 64 tokens 1024 x 8192 25.5 / 16.8; 128 tokens 1024 x 4096 22 / 15.8, 256 x 512 x 8192 37 / 17; 256 x 1024 x 2048 13.0 / 16.3, 128 x 8192 x 4096 22 / 30).
+// The second kernel's grid has the tokens and matrices for dimensions.
 int plan_gated_splits(int64_t M, int64_t F, int64_t rowbytes, int64_t batch)
 {
+    const bool few = M <= kGatedFew;
     const int64_t nslabs = (rowbytes + kSlabBytes - 1) / kSlabBytes;
-    if (nslabs < (M <= kGatedFew ? 48 : 16) || M > 65535 || batch > 65535) return 1;
-    const int64_t blocks = M <= kGatedFew ? (F + 15) / 16 * batch : ((M + 127) / 128) * ((F + 63) / 64) * batch;
-    if (blocks >= 256) return 1;
-    const int64_t splits = std::min<int64_t>(512 / blocks, nslabs / 8);
+    if (nslabs < (few ? 48 : 24) || M > 65535 || batch > 65535) return 1;
+    const int64_t blocks = few ? (F + 15) / 16 * batch : ((M + 127) / 128) * ((F + 63) / 64) * batch;
+    if (blocks >= (few ? 256 : 33)) return 1;
+    const int64_t splits = std::min<int64_t>((few ? 512 : 256) / blocks, nslabs / 8);
     return splits >= 2 ? (int)splits : 1;
 }
 
@@ -2849,6 +3049,19 @@ qmm_status launch_fuse(GemmArgs& g, hipStream_t s)
 }
 
 template <int KIND, int FA, int FB>
+qmm_status launch_gated_deep(GemmArgs& g, hipStream_t s)
+{
+    constexpr int LDS_BYTES = kGatedSlots * (64 + 128) * kSlabBytes;
+    g.tiles_m = (int)((g.F + 31) / 32);
+    g.tiles_n = (int)((g.N + 127) / 128);
+    auto kern = gated_deep_kernel<KIND, FA, FB>;
+    static std::atomic<uint64_t> lds_attr_done{0};
+    if (!ensure_lds_attr(lds_attr_done, reinterpret_cast<const void*>(kern), LDS_BYTES)) return QMM_ERR_LAUNCH;
+    kern<<<(unsigned)((int64_t)g.tiles_m * g.tiles_n * g.batch), 256, LDS_BYTES, s>>>(g);
+    return launch_status();
+}
+
+template <int KIND, int FA, int FB>
 qmm_status launch_gated_few(GemmArgs& g, hipStream_t s)
 {
     const int64_t blocks = (g.F + 15) / 16, total = blocks * g.batch;
@@ -2876,6 +3089,10 @@ qmm_status launch_gated(GemmArgs& g, hipStream_t s)
     if constexpr (KIND != KIND_I8) {
         if (use_stream(g, 0) && g.F <= kGatedColumns) return launch_stream<KIND, FA, FB, 1>(g, s);
     }
+    const int64_t tiles = ((g.N + 127) / 128) * ((g.F + 31) / 32) * g.batch;
+    // (128 x 128 tiles / gated_deep_kernel: E4M3 100 tokens 4096 x 1024, 128 tiles, 11.8 / 9.7 us, 512 x 1024 x 1024 9.7 / 8.5, 300 x 300 x 288 10.7 / 6.7, INT8 1024 x 1024
+    // x 512, 256 tiles, 8.3 / 6.9, bfloat16 512 x 1024 x 1024, 16 slabs, 13.3 / 12.5; 512 tiles 10.7 / 11.2; 32 slabs 22.4 / 23.3)
+    if (tiles <= 256 && g.rowbytes <= 16 * kSlabBytes) return launch_gated_deep<KIND, FA, FB>(g, s);
     const int64_t big = ((g.N + 255) / 256) * ((g.F + 127) / 128) * g.batch;
     const int64_t small = ((g.N + 127) / 128) * ((g.F + 63) / 64) * g.batch;
     const bool narrow = g.N <= 128 || g.F <= 64;
