@@ -341,10 +341,10 @@ typedef enum { QMM_ACT_SILU = 0, QMM_ACT_GELU = 1 } qmm_activation;
  *   h          device [batch][M][F] of out_dtype, rounded once.
  *   gu         device [batch][M][2 F] of out_dtype: g and u, rounded once (h is of the unrounded ones), for
  *              qmm_gated_backward; or NULL.
- *   workspace  qmm_gemm_gated_workspace_size() bytes, 16-byte aligned (0: may be NULL).  K is split as in qmm_gemm where M
- *              and F are small; the parts are added in a fixed order.
+ *   workspace  qmm_gemm_gated_workspace_size() bytes, 16-byte aligned (0: may be NULL).  It is non-zero where M and F are small
+ *              and K long: K is then split and the parts are added in a fixed order.
  * e^-g and Phi are evaluated in binary32 to a few units of the last place (relative to |g| 2^-23 where e^-g is far from 1).
- * A gate of -infinity gives NaN.  Other rules and errors as for qmm_gemm.
+ * A gate of -infinity gives NaN.  F up to 2^22, else QMM_ERR_UNSUPPORTED.  Other rules and errors as for qmm_gemm.
  */
 size_t qmm_gemm_gated_workspace_size(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K);
 qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K,
@@ -353,7 +353,7 @@ qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t ba
 
 /*
  * qmm_gated_backward -- the backward pass of h = act(g) * u up to the operand of the products behind it:
- *     dg = (dh * u) * act'(g),   du = dh * act(g)        a row's results are (dg | du), 2 F values
+ *     dg = (dh * u) * act'(g),   du = dh * act(g)        a row's results are (dg | du), 2 F values (an infinite gate: NaN)
  * as values (for the weight gradient, whose operand is quantized along the other axis) and as codes with one step size per row
  * (the data gradient's operand [batch][rows][2 F], per_channel = 1, batch_groups = batch): what qmm_scale and qmm_quantize give for the
  * binary32 results.

@@ -215,13 +215,16 @@ QMM_DEV uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, bf2));
 }
 
-// The outputs of one block of 16 (32) tokens, inside the matrix; value(p, half, v) is the descaled accumulator.  A lane's columns are one, two or
+// The outputs of one block of 16 (32) tokens; value(p, half, v) is the descaled accumulator.  A lane's columns are one, two or
 // four units of 16 bytes.  Two lanes (or a quad) trade units until each store holds, of a token, all that the wavefront has: whole 128-byte
 // lines by the 256 x 256 tiles.  (256 workgroups writing nothing but such tiles: 4.6 TB/s; with 64 bytes of a line
 // a wavefront, the layout of the plain product, 2.9, and with 4 or 8 bytes a lane the stores' addresses take longer than all else.)
 // next() is called in front of every unit.  h, gu: token 0 of the block, the wavefront's first column; the block's lane j is token T j.  Streaming stores, as the plain
 // product's of this size (gemm_stream_kernel): kept by the L2 they cost a training step's product 209 us instead of 179.
-template <bool F8, int NP, int T, int ACT, bool BF, bool GU, typename Value, typename Next> QMM_DEV void gated_tokens(uint8_t* h, uint8_t* gu, int64_t F, int lane, Value&& value, Next&& next)
+// whole: the block lies inside the matrix and its rows begin on 16-byte boundaries.  Else rows and columns behind the matrix's are left out and the
+// stores are ordinary ones at element boundaries (rows_left, cols_left: from the block's first token and the wavefront's first column on).
+template <bool F8, int NP, int T, int ACT, bool BF, bool GU, typename Value, typename Next>
+QMM_DEV void gated_tokens(uint8_t* h, uint8_t* gu, int64_t F, bool whole, int rows_left, int cols_left, int lane, Value&& value, Next&& next)
 {
     constexpr int PER = F8 ? 4 : 16, E = BF ? 8 : 4, ES = BF ? 2 : 4;      // columns a pair of blocks, columns and bytes ...
     constexpr int CHUNKS = !F8 && !BF && NP == 2 ? 2 : 1;                  // (eight units: pair by pair)
@@ -254,7 +257,8 @@ template <bool F8, int NP, int T, int ACT, bool BF, bool GU, typename Value, typ
             __builtin_amdgcn_sched_barrier(0);               // (a unit at a time: all at once took more registers than there are)
         }
         const int c0 = unit * E;                             // the unit that this lane stores
-        const uint32_t at = (F8 ? COLS * q + c0 : 32 * (ch + c0 / 16) + 16 * q + c0 % 16) * ES;
+        const int column = F8 ? COLS * q + c0 : 32 * (ch + c0 / 16) + 16 * q + c0 % 16;
+        const uint32_t at = column * ES;
 #pragma unroll
         for (int o = 0; o < (GU ? 3 : 1); ++o) {
             if constexpr (U >= 2) {
@@ -272,14 +276,29 @@ template <bool F8, int NP, int T, int ACT, bool BF, bool GU, typename Value, typ
             uint8_t* base = (o == 0 ? h : gu) + (o == 2 ? F * ES : 0);       // uniform; the lane's part fits 32 bits (kGatedColumns)
             const uint32_t pitch = (uint32_t)(o == 0 ? F : 2 * F) * ES;
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                __builtin_nontemporal_store(u32x4{d[o][i][0], d[o][i][1], d[o][i][2], d[o][i][3]},
-                                            reinterpret_cast<u32x4*>(base + ((uint32_t)(T * ((j & ~(U - 1)) + i)) * pitch + at)));
+            for (int i = 0; i < U; ++i) {
+                const int row = T * ((j & ~(U - 1)) + i);
+                const u32x4 w{d[o][i][0], d[o][i][1], d[o][i][2], d[o][i][3]};
+                uint8_t* p = base + ((uint32_t)row * pitch + at);
+                if (whole) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+                else if (row < rows_left) {
+                    typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+                    if (column + E <= cols_left) *reinterpret_cast<u32x4_any*>(p) = w;
+                    else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (column + e < cols_left) {
+                                if constexpr (BF) reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                                else reinterpret_cast<uint32_t*>(p)[e] = w[e];
+                            }
+                    }
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
-// The same one by one, for tiles at an edge and rows that do not begin at a vector's boundary: column f of token n of matrix `bidx`.
+// The same one by one: column f of token n of matrix `bidx`.
 QMM_DEV void gated_one(const GemmArgs& g, int64_t bidx, int64_t n, int64_t f, float hv, float gv, float uv)
 {
     if (n >= g.N || f >= g.F) return;
@@ -424,6 +443,8 @@ gemm_kernel(GemmArgs g)
         k_end = min((int)g.rowbytes, (first + base + (split < rem ? 1 : 0)) * kSlabBytes);
     }
     const uint8_t* a_tile = A + (m0 * g.rowbytes + k_begin) * A_ES;
+    // GATED: a copied unit of 8 LDS rows lies in one block, of gate or of up; by the 32 x 32 instructions all of a wavefront's do
+    if constexpr (GATED && !F8) { if (wave & 1) a_tile += g.F * g.rowbytes; }
     const uint8_t* b_tile = B + (n0 * g.rowbytes + k_begin) * B_ES;
     uint32_t a_src[A_PER_WAVE], b_src[B_PER_WAVE];
     const int lane_chunk_base = lane & 7;
@@ -447,13 +468,9 @@ gemm_kernel(GemmArgs g)
         row = n0 + row < g.N ? row : g.N - 1 - n0;
         b_src[i] = (uint32_t)((row * g.rowbytes + c * 16) * B_ES);
     }
-    // GATED: a copied unit of 8 LDS rows lies in one block, of gate or of up
     auto a_half = [&](int i) -> const uint8_t* {
-        if constexpr (GATED) {
-            static_assert(A_PER_WAVE * 8 == 32, "a wavefront copies two blocks of 16 rows or one of 32");
-            if (F8 ? i >= A_PER_WAVE / 2 : (wave & 1) != 0) return a_tile + g.F * g.rowbytes;
-        }
-        return a_tile;
+        static_assert(!GATED || A_PER_WAVE * 8 == 32, "a wavefront copies two blocks of 16 rows or one of 32");
+        return GATED && F8 && i >= A_PER_WAVE / 2 ? a_tile + g.F * g.rowbytes : a_tile;
     };
 
     // Copy number i of this wavefront for the A (B) slab at byte k0 into ring slot `slot`.
@@ -849,38 +866,19 @@ gemm_kernel(GemmArgs g)
                     }
             return;
         }
-        if (m0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0 && g.F <= kGatedColumns) {
-            const int es = g.y_bf16 ? 2 : 4;
-            gated_forms(g, [&](auto act, auto bf, auto kept) {
-#pragma unroll
-                for (int tt = 0; tt < TILES_N; ++tt) {
-                    uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.N + n_base + tt) * g.F + f_base) * es;
-                    uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.N + n_base + tt) * 2 * g.F + f_base) * es;
-                    gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
-                        h, gu, g.F, lane, [&](int p, int half, int v) { return gated_value(p, half, v, tt); }, next);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            });
-            return;
-        }
-        auto edge = [&](auto act) {
+        const bool whole = m0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0;
+        const int rows_left = (int)min(g.N - n_base, (int64_t)WN), cols_left = (int)min(g.F - f_base, (int64_t)WM);
+        const int es = g.y_bf16 ? 2 : 4;
+        gated_forms(g, [&](auto act, auto bf, auto kept) {
 #pragma unroll
             for (int tt = 0; tt < TILES_N; ++tt) {
-                if (n_base + tt < g.N) {
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
-#pragma unroll
-                        for (int v = 0; v < REGS; ++v) {
-                            bool up;
-                            const int64_t f = f_base + gated_row<F8, NP>(2 * p * R + row_in_block(v), up);
-                            const float gv = gated_value(p, 0, v, tt), uv = gated_value(p, 1, v, tt);
-                            gated_one(g, bidx, n + tt, f, activate<decltype(act)::value>(gv) * uv, gv, uv);
-                        }
-                }
+                uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.N + n_base + tt) * g.F + f_base) * es;
+                uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.N + n_base + tt) * 2 * g.F + f_base) * es;
+                gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
+                    h, gu, g.F, whole, rows_left - tt, cols_left, lane, [&](int p, int half, int v) { return gated_value(p, half, v, tt); }, next);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        if (g.act == QMM_ACT_SILU) edge(std::integral_constant<int, QMM_ACT_SILU>{}); else edge(std::integral_constant<int, QMM_ACT_GELU>{});
+        });
         return;
     }
 
@@ -1819,7 +1817,7 @@ gemm_stream_kernel(GemmArgs g)
                         uint8_t* h = static_cast<uint8_t*>(g.y) + ((cur.bidx * g.N + n_base + tt) * g.F + m_base) * es;
                         uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((cur.bidx * g.N + n_base + tt) * 2 * g.F + m_base) * es;
                         gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
-                            h, gu, g.F, lane_e, [&](int p, int half, int v) { return value(2 * p + half, v, tt); }, next);
+                            h, gu, g.F, true, 0, 0, lane_e, [&](int p, int half, int v) { return value(2 * p + half, v, tt); }, next);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 });
@@ -2568,32 +2566,18 @@ gated_deep_kernel(GemmArgs g)
         if constexpr (descale) a = (a * st[tt]) * sw[p][half][v];
         return a;
     };
-    if (f0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0 && g.F <= kGatedColumns) {
-        const int es = g.y_bf16 ? 2 : 4;
-        gated_forms(g, [&](auto act, auto bf, auto kept) {
+    const bool whole = f0 + BM / 2 <= g.F && n0 + BN <= g.N && g.F % 8 == 0;
+    const int rows_left = (int)min(g.N - n_base, (int64_t)WN), cols_left = (int)min(g.F - f0, (int64_t)BM);
+    const int es = g.y_bf16 ? 2 : 4;
+    gated_forms(g, [&](auto act, auto bf, auto kept) {
 #pragma unroll
-            for (int tt = 0; tt < TILES_N; ++tt) {
-                uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.N + n_base + tt) * g.F + f0) * es;
-                uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.N + n_base + tt) * 2 * g.F + f0) * es;
-                gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
-                    h, gu, g.F, lane, [&](int p, int half, int v) { return value(p, half, v, tt); }, []() {});
-            }
-        });
-        return;
-    }
-    auto edge = [&](auto act) {
-#pragma unroll
-        for (int tt = 0; tt < TILES_N; ++tt)
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int v = 0; v < REGS; ++v) {
-                    bool up;
-                    const float gv = value(p, 0, v, tt), uv = value(p, 1, v, tt);
-                    gated_one(g, bidx, n + tt, column(p, v, up), activate<decltype(act)::value>(gv) * uv, gv, uv);
-                }
-    };
-    if (g.act == QMM_ACT_SILU) edge(std::integral_constant<int, QMM_ACT_SILU>{}); else edge(std::integral_constant<int, QMM_ACT_GELU>{});
+        for (int tt = 0; tt < TILES_N; ++tt) {
+            uint8_t* h = static_cast<uint8_t*>(g.y) + ((bidx * g.N + n_base + tt) * g.F + f0) * es;
+            uint8_t* gu = static_cast<uint8_t*>(g.gu) + ((bidx * g.N + n_base + tt) * 2 * g.F + f0) * es;
+            gated_tokens<F8, NP, TILES_N, decltype(act)::value, decltype(bf)::value, decltype(kept)::value>(
+                h, gu, g.F, whole, rows_left - tt, cols_left, lane, [&](int p, int half, int v) { return value(p, half, v, tt); }, []() {});
+        }
+    });
 }
 
 // A gated product of few tokens (at most 64): it takes as long as its weights are on their way from memory, 2 F K codes, so the point is to have
@@ -3087,7 +3071,7 @@ qmm_status launch_gated(GemmArgs& g, hipStream_t s)
     // epilogue has no registers left beside the stream's (spilled, 190 against 187).
     if (g.splits > 1) return launch_tile<KIND, FA, FB, 2, 1, 2, 0, 0, 1>(g, s);
     if constexpr (KIND != KIND_I8) {
-        if (use_stream(g, 0) && g.F <= kGatedColumns) return launch_stream<KIND, FA, FB, 1>(g, s);
+        if (use_stream(g, 0)) return launch_stream<KIND, FA, FB, 1>(g, s);
     }
     const int64_t tiles = ((g.N + 127) / 128) * ((g.F + 31) / 32) * g.batch;
     // (128 x 128 tiles / gated_deep_kernel: E4M3 100 tokens 4096 x 1024, 128 tiles, 11.8 / 9.7 us, 512 x 1024 x 1024 9.7 / 8.5, 300 x 300 x 288 10.7 / 6.7, INT8 1024 x 1024
@@ -3311,7 +3295,7 @@ extern "C" qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b,
     if (!h || (!bf && (!a->delta || !b->delta))) return QMM_ERR_NULL;
     const int64_t esz = bf ? 2 : 1;
     if ((K * esz) % 16 != 0) return QMM_ERR_ALIGN;
-    if (K * esz > (int64_t(1) << 22)) return QMM_ERR_UNSUPPORTED;   // the kernels keep 32-bit byte offsets within a tile's rows
+    if (K * esz > (int64_t(1) << 22) || F > kGatedColumns) return QMM_ERR_UNSUPPORTED;   // the kernels keep 32-bit byte offsets within a tile's rows
     if (K > 0 && (!a->data || !b->data)) return QMM_ERR_NULL;
     if (!aligned16(a->data) || !aligned16(b->data) || !aligned16(h) || !aligned16(gu)) return QMM_ERR_ALIGN;
 

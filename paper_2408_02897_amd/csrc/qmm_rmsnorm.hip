@@ -451,6 +451,8 @@ extern "C" qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor
     for (const void* out : {static_cast<const void*>(h_out), static_cast<const void*>(y_out)})      // over an input: element by element only
         if (out && ((out == x->data && !dense(x)) || (residual && out == residual->data && !dense(residual)))) return QMM_ERR_SHAPE;
 
+    if (h_out && h_out == y_out && x->cols > 0) return QMM_ERR_SHAPE;
+
     NormArgs a{};
     a.x = x->data; a.x_batch = x->batch_stride; a.x_row = x->row_stride;
     if (residual) { a.r = residual->data; a.r_batch = residual->batch_stride; a.r_row = residual->row_stride; a.h = h_out; }

@@ -156,7 +156,8 @@ inline bool dense(const qmm_tensor* t)
 {
     return (t->rows <= 1 || t->row_stride == t->cols) && (t->batch <= 1 || t->batch_stride == t->rows * t->cols);
 }
-inline unsigned row_blocks(int64_t total, int per) { return (unsigned)std::min<int64_t>((total + per - 1) / per, 0x7FFFFFFF); }
+// workgroups for `total` rows, `per` each (they go round where the grid would pass what a launch takes, 2^32 threads)
+inline unsigned row_blocks(int64_t total, int per) { return (unsigned)std::min<int64_t>((total + per - 1) / per, 1 << 21); }
 
 }  // namespace
 }  // namespace qmm

@@ -66,6 +66,7 @@ def test_norm_refusals(L):
         assert fwd(T(), T(), **{**dict(h=p), k: off}) == 4
     assert fwd(T(data=0x20002)) == 4
     assert fwd(T(rs=20, bs=80), T(), h=ctypes.c_void_p(0x20000)) == 2           # over an input whose rows lie apart
+    assert fwd(T(), T(data=0x30000), h=p, y=p) == 2
     assert fwd(T(b=0), d=None, c=None) == 0 and fwd(T(r=0, data=None), d=None, c=None) == 0
 
     need = L.qmm_rmsnorm_backward_workspace_size(ref(T()))
@@ -96,7 +97,7 @@ def test_gated_refusals(L):
     assert run(O(), O(fmt=qmm.INT8)) == 5 and run(O(), O(fmt=qmm.BF16, codes=0)) == 5 and run(O(codes=0), O()) == 5 and run(O(), O(codes=0)) == 5
     assert run(O(), O(), n=(1, -8, 16, 32)) == 2 and run(O(), O(), n=(1, 8, -1, 32)) == 2 and run(O(), O(), n=(-1, 8, 16, 32)) == 2
     assert run(O(), O(), n=(1, 8, 16, 24)) == 4 and run(O(data=off), O()) == 4 and run(O(), O(), h=off) == 4 and run(O(), O(), gu=off) == 4
-    assert run(O(), O(), n=(1, 8, 16, (1 << 22) + 16)) == 5
+    assert run(O(), O(), n=(1, 8, 16, (1 << 22) + 16)) == 5 and run(O(), O(), n=(1, 8, (1 << 22) + 1, 32)) == 5
     for n in ((0, 8, 16, 32), (1, 0, 16, 32), (1, 8, 0, 32)):
         assert run(O(data=None), O(), n=n, h=None) == 0 and L.qmm_gemm_gated_workspace_size(ref(O()), ref(O()), *n) == 0
     assert L.qmm_gemm_gated_workspace_size(None, ref(O()), 1, 8, 16, 32) == 0
