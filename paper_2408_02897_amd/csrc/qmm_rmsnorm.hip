@@ -27,7 +27,7 @@ struct NormArgs {
     int64_t batch, rows, cols;
     uint64_t seed, offset;
     float qmax; int fmt;
-    int streaming;                             // h and y go past the caches (host)
+    int streaming, x_streaming;                // h and y go past the caches; so do x and r (host)
 };
 
 // 1 / sqrt(mean + eps), both operations correctly rounded
@@ -54,21 +54,20 @@ rmsnorm_rows(NormArgs a)
         const T* x = static_cast<const T*>(a.x) + b * a.x_batch + i * a.x_row;
         u32x4 w[NV];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) w[k] = load_row<T>(x + c0 + k * LPR * V, cols - c0 - k * LPR * V);
+        for (int k = 0; k < NV; ++k) w[k] = load_row<T>(x + c0 + k * LPR * V, cols - c0 - k * LPR * V, a.x_streaming);
         if (a.r) {
             const T* r = static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row;
             T* h = static_cast<T*>(a.h) + id * a.cols;
             u32x4 q[NV];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) q[k] = load_row<T>(r + c0 + k * LPR * V, cols - c0 - k * LPR * V);
+            for (int k = 0; k < NV; ++k) q[k] = load_row<T>(r + c0 + k * LPR * V, cols - c0 - k * LPR * V, a.x_streaming);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float v[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = Vec<T>::at(w[k], e) + Vec<T>::at(q[k], e);
                 w[k] = pack_row<T>(v);
-                if (a.streaming) stream_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
-                else store_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
+                store_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V, a.streaming);
             }
         }
         float y[NV][V], sum = 0.0f;
@@ -100,10 +99,7 @@ rmsnorm_rows(NormArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) y[k][e] *= rstd;
             const int64_t p = id * a.cols + c;
-            if (a.y) {
-                if (a.streaming) stream_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
-                else store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
-            }
+            if (a.y) store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left, a.streaming);
             store_codes<T>(a.codes + p, encode_values<V, MODE>(y[k], rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
         }
     }
@@ -173,6 +169,7 @@ struct NormGradArgs {
     const float* rstd;
     const void* w; int w_bf16;
     void* dx;
+    int streaming;                                     // dy, h and r are read by streaming loads (host)
     float* partial;                                    // [gridDim.x][cols] shares of dw, or null
     float* dw;
     int64_t batch, rows, cols;
@@ -211,10 +208,10 @@ rmsnorm_grad_rows(NormGradArgs a)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * LPR * V;
-            r.g[k] = load_row<T>(dy + c, cols - c);
-            r.w[k] = load_row<T>(h + c, cols - c);
+            r.g[k] = load_row<T>(dy + c, cols - c, a.streaming);
+            r.w[k] = load_row<T>(h + c, cols - c, a.streaming);
             r.q[k] = u32x4{0u, 0u, 0u, 0u};
-            if (a.r) r.q[k] = load_row<T>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row + c, cols - c);
+            if (a.r) r.q[k] = load_row<T>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row + c, cols - c, a.streaming);
         }
         r.rstd = live ? a.rstd[id] : 0.0f;
     };
@@ -464,6 +461,8 @@ extern "C" qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor
     // h is wanted by the next addition to the residual stream, y by the backward pass: from where they would fill the caches between here and there
     // they go past them, the codes, which the next product reads, do not (bfloat16 16384 x 4096 with y 115 -> 108 us, 8192 x 8192 97 -> 90,
     // binary32 16384 x 4096 168 -> 154; 16384 x 1024, 33 MB, 22.7 -> 22.2)
+    // Reading x and the residual by streaming loads as well: 108 -> 102 and 90 -> 86; 16384 x 1024 22.5 -> 25.1.
+    a.x_streaming = residual && streams(x) && streams(residual);
     a.streaming = a.batch * a.rows * a.cols * (x->dtype == QMM_DT_BF16 ? 2 : 4) >= (int64_t)64 << 20;
     hipStream_t s = as_stream(stream);
     if (x->dtype == QMM_DT_BF16)
@@ -518,5 +517,6 @@ extern "C" qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tenso
     a.h = h->data; a.h_batch = h->batch_stride; a.h_row = h->row_stride;
     if (dresidual) { a.r = dresidual->data; a.r_batch = dresidual->batch_stride; a.r_row = dresidual->row_stride; }
     a.rstd = rstd; a.w = weight; a.w_bf16 = weight_dtype == QMM_DT_BF16; a.dx = dx_out;
+    a.streaming = streams(dy) && streams(h) && (!dresidual || streams(dresidual));       // (bfloat16 16384 x 4096 104 -> 95 us, 8192 x 8192 112 -> 108)
     return dy->dtype == QMM_DT_BF16 ? launch_norm_grad<uint16_t>(a, s) : launch_norm_grad<float>(a, s);
 }

@@ -394,6 +394,50 @@ def test_gated_backward_special_rows():
         near(v[4, :40], dh[4].double() * gu[4, 40:].double() * far, 1e-5 * (dh[4] * gu[4, 40:]).abs().double())
 
 
+# ------------------------------------------------------------------------------------------------ large tensors
+@pytest.mark.parametrize("rows,cols,dtype", [(8192, 4096, BF), (8200, 4104, BF), (4096, 4096, F32), (600000, 3600, BF)])
+def test_large_rows_equal_small_calls(rows, cols, dtype):
+    """From 64 MB on tensors are read and written past the caches; the last one has more than 2^31 elements.  A row's results do not depend on the others."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    x = torch.randn((rows, cols), generator=g, device=DEV, dtype=dtype)
+    w = torch.rand(cols, generator=g, device=DEV) + 0.5
+    some = [slice(0, 70), slice(rows // 2, rows // 2 + 70), slice(rows - 70, rows)]
+    r = x.flip(0) if rows < 100000 else None
+    n = qmm.rmsnorm_quantize(x, w, qmm.E4M3, residual=r, want_y=True, want_rstd=True)
+    for k in some:
+        m = qmm.rmsnorm_quantize(x[k], w, qmm.E4M3, residual=None if r is None else r[k].contiguous(), want_y=True, want_rstd=True)
+        assert R.same_bits(n.codes[:, k].contiguous(), m.codes) and R.same_bits(n.delta[k], m.delta) and R.same_bits(n.h[k], m.h) and R.same_bits(n.y[k], m.y) and R.same_bits(n.rstd[k], m.rstd)
+    dx, dw = qmm.rmsnorm_backward(n.y, n.h, n.rstd, w, dresidual=r)
+    for k in some:
+        assert R.same_bits(dx[k], qmm.rmsnorm_backward(n.y[k], n.h[k], n.rstd[k], w, dresidual=None if r is None else r[k].contiguous(), want_dw=False)[0])
+    want, size = torch.zeros(cols, dtype=torch.float64, device=DEV), torch.zeros(cols, dtype=torch.float64, device=DEV)
+    for k in range(0, rows, 20000):
+        t = n.y[k:k + 20000].double() * (n.h[k:k + 20000].double() * n.rstd[k:k + 20000].double().unsqueeze(1))
+        want += t.sum(0); size += t.abs().sum(0)
+    # a share adds rows / 512 products one behind the other, the fold some thirty shares: (1172 + 40 + 2) 2^-24 at most
+    assert torch.all((dw.double() - want).abs() <= 2.0 ** -13 * size)
+    del dx, r
+    if rows < 100000:
+        gu = torch.randn((rows, 2 * cols), generator=g, device=DEV, dtype=dtype)
+        d = qmm.gated_backward(x, gu, qmm.SILU, qmm.E5M2, want_dgu=True)
+        for k in some:
+            e = qmm.gated_backward(x[k], gu[k], qmm.SILU, qmm.E5M2, want_dgu=True)
+            assert R.same_bits(d.codes[:, k].contiguous(), e.codes) and R.same_bits(d.delta[k], e.delta) and R.same_bits(d.dgu[k], e.dgu)
+
+
+@pytest.mark.parametrize("m,f", [(66048, 32896), (66001, 33001)])
+def test_gated_product_past_32_bits(m, f):
+    """More than 2^31 outputs, by the kernel whose workgroups stay and by the other one."""
+    a = (torch.randn((m, 384), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)).to(torch.float8_e4m3fn).view(torch.uint8)
+    w = (torch.randn((2 * f, 384), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV) * 0.05).to(torch.float8_e4m3fn).view(torch.uint8)
+    da, dw = torch.rand(m, device=DEV) + 0.5, torch.rand(2 * f, device=DEV) + 0.5
+    op = lambda t, d: (t, qmm.operand(t, qmm.E4M3, d, per_channel=True))
+    h = qmm.gemm_gated(op(a, da), op(w, dw))[0]
+    for k in (slice(0, 300), slice(m - 300, m)):
+        small = qmm.gemm_gated(op(a[k].contiguous(), da[k].contiguous()), op(w, dw))[0]
+        assert R.same_bits(h[k], small)
+
+
 # ------------------------------------------------------------------------------------------------ together
 def test_native_calls_equal_the_ctypes_ones(monkeypatch):
     x, r, w = normal(1, 2, 30, 100, dtype=BF).to(DEV), normal(2, 2, 30, 100, dtype=BF).to(DEV), normal(3, 100).to(DEV)
