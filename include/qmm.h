@@ -10,6 +10,11 @@
  *                 descale by deltaL * deltaR                        (Methodology, scaling bullet)
  *   qmm_metric    error sums of the result against the high-precision
  *                 product: noise-to-signal ratio, Eq. 2, Eq. 3      (Results, Eq. 2 and Eq. 3)
+ * and, for the products of a transformer's feed-forward block, what stands around them
+ * (extensions: the paper quantizes the products, it does not say what feeds them):
+ *   qmm_rmsnorm_quantize   residual addition, root-mean-square norm, steps 1 and 2 in one pass
+ *   qmm_gemm_gated         both projections, activation and product in one kernel
+ *   qmm_gated_backward, qmm_rmsnorm_backward   their gradients, the first one quantized
  *
  * General rules
  *  - Every pointer named "device" is GPU memory owned by the caller; the
