@@ -326,7 +326,7 @@ qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor* residual,
  *   rstd               device, batch * rows floats, as qmm_rmsnorm_quantize wrote it.
  *   dx_out             device, dense, their type; may be the memory of one of them where that is dense.
  *   dw_out             device, cols floats, or NULL.  Sums in binary32 in an order fixed by the extents.
- *   workspace          qmm_rmsnorm_backward_workspace_size(dy) bytes, 16-byte aligned; not needed without dw_out.
+ *   workspace          qmm_rmsnorm_backward_workspace_size(dy) bytes, 16-byte aligned (0: may be NULL); not needed without dw_out.
  * Errors as above; without rows dw is zero.
  */
 size_t qmm_rmsnorm_backward_workspace_size(const qmm_tensor* dy);

@@ -89,14 +89,14 @@ def check_asm():
     with ThreadPoolExecutor(max_workers=GEMM_PARTS) as ex:
         text = "\n".join(ex.map(assemble, range(GEMM_PARTS)))
     findings = []
-    names = list(dict.fromkeys(re.findall(r"^(_ZN3qmm\S*(?:gemm_kernel|gemm_shortk_kernel|gemm_stream_kernel|gemm_deep_kernel|gemm_direct_kernel)\S*):", text, flags=re.M)))
+    names = list(dict.fromkeys(re.findall(r"^(_ZN3qmm\S*(?:gemm_kernel|gemm_shortk_kernel|gemm_stream_kernel|gemm_deep_kernel|gemm_direct_kernel|gated_deep_kernel|gated_few_kernel)\S*):", text, flags=re.M)))
     for nm in names:
         start = text.index("\n" + nm + ":")
         end = text.index(".Lfunc_end", start)
         body = text[start:end]
         instrs = [l.strip() for l in body.split("\n")
                   if l.strip() and not l.strip().startswith((";", ".")) and not l.strip().endswith(":")]
-        by_builtin = "gemm_deep_kernel" in nm or "gemm_direct_kernel" in nm       # the compiler knows these matrix instructions
+        by_builtin = any(k in nm for k in ("gemm_deep_kernel", "gemm_direct_kernel", "gated_deep_kernel", "gated_few_kernel"))       # the compiler knows these matrix instructions
         for k, l in enumerate([] if by_builtin else instrs):
             m = re.match(r"v_mfma\S+ a\[(\d+):(\d+)\]", l)
             if not m:

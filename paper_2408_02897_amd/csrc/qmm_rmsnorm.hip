@@ -371,11 +371,11 @@ rmsnorm_grad_fold(NormGradArgs a)
 
 // Shares of dw: workgroups that go over rows, of columns' parts of rows where rows are long.  Two workgroups a CU, one of 1024 threads: enough to keep
 // the rows coming, and every further one is a share more to write and fold (bfloat16 16384 x 4096, 256 / 384 / 512 / 768 / 1024 workgroups 135 / 109 / 104 / 108 /
-// 119 us; binary32 1000 x 12000, 1024 threads, 256 / 512: 53 / 61).
+// 119 us; binary32 1000 x 12000, 1024 threads, 256 / 512: 53 / 61).  Where up to four would work one does, and its share is dw: no fold, no workspace.
 int64_t shares_of(const qmm_tensor* t)
 {
     const int64_t total = t->batch * t->rows;
-    if (t->cols > kRowElements) return std::min<int64_t>(total, 64);
+    if (t->cols > kRowElements) return total <= 4 ? 1 : std::min<int64_t>(total, 64);
     int64_t blocks = 0, most = 512;
     auto count = [&](auto lpr, auto) {
         constexpr int rpb = lpr.value < 256 ? 256 / lpr.value : 1;
@@ -383,7 +383,7 @@ int64_t shares_of(const qmm_tensor* t)
         if (lpr.value == 1024) most = 256;
     };
     if (t->dtype == QMM_DT_BF16) for_row_size<uint16_t>(t->cols, count); else for_row_size<float>(t->cols, count);
-    return std::min(blocks, most);
+    return blocks <= 4 ? 1 : std::min(blocks, most);
 }
 
 template <typename T, int MODE> qmm_status launch_norm(const NormArgs& a, hipStream_t s)
@@ -412,7 +412,7 @@ template <typename T> qmm_status launch_norm_grad(NormGradArgs& a, hipStream_t s
             rmsnorm_grad_rows<T, lpr.value, nv.value><<<(unsigned)a.shares, threads, 0, s>>>(a);
         });
     }
-    if (a.partial) {
+    if (a.partial && a.partial != a.dw) {
         if (hipGetLastError() != hipSuccess) return QMM_ERR_LAUNCH;
         rmsnorm_grad_fold<<<(unsigned)((a.cols + 15) / 16), 1024, 0, s>>>(a);
     }
@@ -475,7 +475,8 @@ extern "C" qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor
 extern "C" size_t qmm_rmsnorm_backward_workspace_size(const qmm_tensor* dy)
 {
     if (!dy || check_rows(dy) != QMM_OK || dy->batch * dy->rows * dy->cols == 0) return 0;
-    return (size_t)shares_of(dy) * (size_t)dy->cols * sizeof(float);
+    const int64_t shares = shares_of(dy);
+    return shares > 1 ? (size_t)shares * (size_t)dy->cols * sizeof(float) : 0;
 }
 
 extern "C" qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tensor* h, const float* rstd, const void* weight, qmm_dtype weight_dtype,
@@ -504,9 +505,13 @@ extern "C" qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tenso
     if (!element_aligned(dx_out, dy->dtype) || !element_aligned(weight, weight_dtype) || !element_aligned(rstd, QMM_DT_F32) ||
         !element_aligned(dw_out, QMM_DT_F32)) return QMM_ERR_ALIGN;
     if (dw_out && !empty) {
-        if (!workspace || workspace_bytes < qmm_rmsnorm_backward_workspace_size(dy)) return QMM_ERR_WORKSPACE;
-        if (!aligned16(workspace)) return QMM_ERR_ALIGN;
-        a.partial = static_cast<float*>(workspace);
+        const size_t need = qmm_rmsnorm_backward_workspace_size(dy);
+        a.partial = dw_out;                                  // a single share
+        if (need > 0) {
+            if (!workspace || workspace_bytes < need) return QMM_ERR_WORKSPACE;
+            if (!aligned16(workspace)) return QMM_ERR_ALIGN;
+            a.partial = static_cast<float*>(workspace);
+        }
     }
     a.dw = dw_out;
     hipStream_t s = as_stream(stream);

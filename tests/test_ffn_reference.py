@@ -69,7 +69,9 @@ def test_norm_refusals(L):
     assert fwd(T(), T(data=0x30000), h=p, y=p) == 2
     assert fwd(T(b=0), d=None, c=None) == 0 and fwd(T(r=0, data=None), d=None, c=None) == 0
 
-    need = L.qmm_rmsnorm_backward_workspace_size(ref(T()))
+    assert L.qmm_rmsnorm_backward_workspace_size(ref(T())) == 0                   # few rows: one share, which is dw
+    many = dict(r=400, bs=6400)
+    need = L.qmm_rmsnorm_backward_workspace_size(ref(T(**many)))
     assert need > 0 and need % 64 == 0 and L.qmm_rmsnorm_backward_workspace_size(ref(T(rs=8))) == 0 and L.qmm_rmsnorm_backward_workspace_size(None) == 0
 
     def bwd(dy, h, r=None, rstd=p, w=p, wt=qmm.DT_F32, dx=p, dw=p, ws=p, nws=1 << 20):
@@ -78,7 +80,7 @@ def test_norm_refusals(L):
     assert bwd(T(data=None), T()) == 1 and bwd(T(), T(data=None)) == 1 and bwd(T(), T(), T(data=None)) == 1
     assert bwd(T(), T(c=8)) == 2 and bwd(T(), T(), T(r=5, bs=80)) == 2 and bwd(T(), T(dtype=qmm.DT_BF16)) == 5 and bwd(T(), T(axis=0)) == 5
     assert bwd(T(), T(), wt=4) == 3 and bwd(T(), T(), rstd=off) == 4 and bwd(T(), T(), dw=off) == 4 and bwd(T(), T(), dx=off) == 4
-    assert bwd(T(), T(), ws=None) == 6 and bwd(T(), T(), nws=need - 1) == 6 and bwd(T(), T(), ws=ctypes.c_void_p(0x10004)) == 4
+    assert bwd(T(**many), T(**many), ws=None) == 6 and bwd(T(**many), T(**many), nws=need - 1) == 6 and bwd(T(**many), T(**many), ws=ctypes.c_void_p(0x10004)) == 4
     assert bwd(T(rs=20, bs=80), T(), dx=ctypes.c_void_p(0x20000)) == 2
     assert bwd(T(c=0, rs=0), T(c=0, rs=0)) == 0
 
