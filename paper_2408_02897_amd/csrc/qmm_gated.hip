@@ -18,7 +18,6 @@ struct GatedGradArgs {
     int64_t batch, rows, F;
     uint64_t seed, offset;
     float qmax; int fmt;
-    int streaming;                             // dh and gu are read, dgu is written past the caches (host)
 };
 
 // V pairs of results
@@ -33,13 +32,14 @@ template <typename T, int ACT> QMM_DEV void gated_grad(const u32x4& dh, const u3
         du[e] = d * value;
     }
 }
-template <typename T, int MODE> QMM_DEV void gated_grad_out(const GatedGradArgs& a, int64_t p, const float* v, int left, float rho)
+template <typename T, int MODE, bool STREAM> QMM_DEV void gated_grad_out(const GatedGradArgs& a, int64_t p, const float* v, int left, float rho)
 {
-    if (a.dgu) store_row<T>(static_cast<T*>(a.dgu) + p, pack_row<T>(v), left, a.streaming);
-    if (a.codes) store_codes<T>(a.codes + p, encode_values<Vec<T>::V, MODE>(v, rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
+    if (a.dgu) put_row<T, STREAM>(static_cast<T*>(a.dgu) + p, pack_row<T>(v), left);
+    if (a.codes) store_row_codes<T>(a.codes + p, encode_values<Vec<T>::V, MODE>(v, rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
 }
 
-template <typename T, int MODE, int ACT, int LPR, int NV> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
+// STREAM: dh and gu are read, dgu is written past the caches (host).
+template <typename T, int MODE, int ACT, int LPR, int NV, bool STREAM> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
 gated_grad_rows(GatedGradArgs a)
 {
     constexpr int V = Vec<T>::V, THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
@@ -58,15 +58,16 @@ gated_grad_rows(GatedGradArgs a)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * LPR * V;
-            wd[k] = load_row<T>(dh + c, F - c, a.streaming);
-            wg[k] = load_row<T>(g + c, F - c, a.streaming);
-            wu[k] = load_row<T>(g + a.F + c, F - c, a.streaming);
+            wd[k] = fetch_row<T, LPR == 8, STREAM>(dh, c, F);
+            wg[k] = fetch_row<T, LPR == 8, STREAM>(g, c, F);
+            wu[k] = fetch_row<T, LPR == 8, STREAM>(g + a.F, c, F);
         }
         float dg[NV][V], du[NV][V], none = 0.0f;
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            gated_grad<T, ACT>(wd[k], wg[k], wu[k], dg[k], du[k]);
+            const int c = c0 + k * LPR * V;
+            gated_grad<T, ACT>(settle_row<T, LPR == 8, STREAM>(wd[k], c, F), settle_row<T, LPR == 8, STREAM>(wg[k], c, F), settle_row<T, LPR == 8, STREAM>(wu[k], c, F), dg[k], du[k]);
 #pragma unroll
             for (int e = 0; e < V; ++e) m = max(m, max(mag_bits(dg[k][e]), mag_bits(du[k][e])));
         }
@@ -79,8 +80,8 @@ gated_grad_rows(GatedGradArgs a)
             const int c = c0 + k * LPR * V, left = F - c;
             if (left <= 0) continue;
             const int64_t p = id * 2 * a.F + c;
-            gated_grad_out<T, MODE>(a, p, dg[k], left, rho);
-            gated_grad_out<T, MODE>(a, p + a.F, du[k], left, rho);
+            gated_grad_out<T, MODE, STREAM>(a, p, dg[k], left, rho);
+            gated_grad_out<T, MODE, STREAM>(a, p + a.F, du[k], left, rho);
         }
     }
 }
@@ -102,7 +103,7 @@ gated_grad_long(GatedGradArgs a)
         if (a.codes) {
             for (int64_t c = (int64_t)threadIdx.x * V; c < a.F; c += kRowLanes * V) {
                 const int left = (int)min((int64_t)V, a.F - c);
-                gated_grad<T, ACT>(load_row<T>(dh + c, left), load_row<T>(g + c, left), load_row<T>(g + a.F + c, left), dg, du);
+                gated_grad<T, ACT>(load_row<T>(dh, (int)c, (int)a.F), load_row<T>(g, (int)c, (int)a.F), load_row<T>(g + a.F, (int)c, (int)a.F), dg, du);
 #pragma unroll
                 for (int e = 0; e < V; ++e) m = max(m, max(mag_bits(dg[e]), mag_bits(du[e])));
             }
@@ -112,27 +113,30 @@ gated_grad_long(GatedGradArgs a)
         if (threadIdx.x == 0 && a.delta) a.delta[id] = d;
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.F; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.F - c);
-            gated_grad<T, ACT>(load_row<T>(dh + c, left), load_row<T>(g + c, left), load_row<T>(g + a.F + c, left), dg, du);
+            gated_grad<T, ACT>(load_row<T>(dh, (int)c, (int)a.F), load_row<T>(g, (int)c, (int)a.F), load_row<T>(g + a.F, (int)c, (int)a.F), dg, du);
             const int64_t p = id * 2 * a.F + c;
-            gated_grad_out<T, MODE>(a, p, dg, left, rho);
-            gated_grad_out<T, MODE>(a, p + a.F, du, left, rho);
+            gated_grad_out<T, MODE, false>(a, p, dg, left, rho);
+            gated_grad_out<T, MODE, false>(a, p + a.F, du, left, rho);
         }
     }
 }
 
-template <typename T, int MODE, int ACT> qmm_status launch_gated_grad(const GatedGradArgs& a, hipStream_t s)
+template <typename T, int MODE, int ACT> qmm_status launch_gated_grad(const GatedGradArgs& a, bool stream, hipStream_t s)
 {
     const int64_t total = a.batch * a.rows;
     if (a.F > kRowElements) gated_grad_long<T, MODE, ACT><<<row_blocks(total, 1), kRowLanes, 0, s>>>(a);
     else for_row_size<T>(a.F, [&](auto lpr, auto nv) {
         constexpr int threads = lpr.value > 256 ? lpr.value : 256;
-        gated_grad_rows<T, MODE, ACT, lpr.value, nv.value><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a);
+        if constexpr (lpr.value >= kWave) {
+            if (stream) { gated_grad_rows<T, MODE, ACT, lpr.value, nv.value, true><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a); return; }
+        }
+        gated_grad_rows<T, MODE, ACT, lpr.value, nv.value, false><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a);
     });
     return launch_status();
 }
-template <typename T, int MODE> qmm_status launch_gated_act(const GatedGradArgs& a, qmm_activation act, hipStream_t s)
+template <typename T, int MODE> qmm_status launch_gated_act(const GatedGradArgs& a, qmm_activation act, bool stream, hipStream_t s)
 {
-    return act == QMM_ACT_SILU ? launch_gated_grad<T, MODE, QMM_ACT_SILU>(a, s) : launch_gated_grad<T, MODE, QMM_ACT_GELU>(a, s);
+    return act == QMM_ACT_SILU ? launch_gated_grad<T, MODE, QMM_ACT_SILU>(a, stream, s) : launch_gated_grad<T, MODE, QMM_ACT_GELU>(a, stream, s);
 }
 
 }  // namespace
@@ -171,9 +175,9 @@ extern "C" qmm_status qmm_gated_backward(const qmm_tensor* dh, const qmm_tensor*
     a.seed = seed; a.offset = offset; a.qmax = host_qmax(fmt); a.fmt = fmt;
     // From 64 MB of dh on, i.e. 128 MB of dgu, half of what the memory-side cache holds: bfloat16 16384 x 4096 142 -> 120 us, binary32 4096 x 8192 133 -> 123
     // (the loads alone 140, 134).
-    a.streaming = streams(dh) && streams(gu);
+    const bool streaming = streams(dh) && streams(gu) && aligned16(dgu_out);
     hipStream_t s = as_stream(stream);
     if (dh->dtype == QMM_DT_BF16)
-        return mode == QMM_ROUND_RTNE ? launch_gated_act<uint16_t, QMM_ROUND_RTNE>(a, act, s) : launch_gated_act<uint16_t, QMM_ROUND_STOCHASTIC>(a, act, s);
-    return mode == QMM_ROUND_RTNE ? launch_gated_act<float, QMM_ROUND_RTNE>(a, act, s) : launch_gated_act<float, QMM_ROUND_STOCHASTIC>(a, act, s);
+        return mode == QMM_ROUND_RTNE ? launch_gated_act<uint16_t, QMM_ROUND_RTNE>(a, act, streaming, s) : launch_gated_act<uint16_t, QMM_ROUND_STOCHASTIC>(a, act, streaming, s);
+    return mode == QMM_ROUND_RTNE ? launch_gated_act<float, QMM_ROUND_RTNE>(a, act, streaming, s) : launch_gated_act<float, QMM_ROUND_STOCHASTIC>(a, act, streaming, s);
 }

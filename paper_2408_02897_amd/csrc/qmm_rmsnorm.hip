@@ -29,7 +29,6 @@ struct NormArgs {
     int64_t batch, rows, cols;
     uint64_t seed, offset;
     float qmax; int fmt;
-    int streaming, x_streaming;                // h and y go past the caches; so do x and r (host)
 };
 
 // 1 / sqrt(mean + eps), both operations correctly rounded
@@ -40,7 +39,8 @@ QMM_DEV float rstd_of(float sum, int64_t cols, float eps)
 }
 
 // Rows of up to kRowElements: LPR lanes hold one, NV vectors a lane.
-template <typename T, int MODE, int LPR, int NV> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
+// STREAM: x and r are read, h and y written past the caches (host).
+template <typename T, int MODE, int LPR, int NV, bool STREAM> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
 rmsnorm_rows(NormArgs a)
 {
     constexpr int V = Vec<T>::V, THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
@@ -56,27 +56,32 @@ rmsnorm_rows(NormArgs a)
         const T* x = static_cast<const T*>(a.x) + b * a.x_batch + i * a.x_row;
         u32x4 w[NV];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) w[k] = load_row<T>(x + c0 + k * LPR * V, cols - c0 - k * LPR * V, a.x_streaming);
+        for (int k = 0; k < NV; ++k) w[k] = fetch_row<T, LPR == 8, STREAM>(x, c0 + k * LPR * V, cols);
         if (a.r) {
             const T* r = static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row;
             T* h = static_cast<T*>(a.h) + id * a.cols;
             u32x4 q[NV];
 #pragma unroll
-            for (int k = 0; k < NV; ++k) q[k] = load_row<T>(r + c0 + k * LPR * V, cols - c0 - k * LPR * V, a.x_streaming);
+            for (int k = 0; k < NV; ++k) q[k] = fetch_row<T, LPR == 8, STREAM>(r, c0 + k * LPR * V, cols);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
+                // (both shifted alike: the sum of the vectors is the vector of the sums)
                 float v[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = Vec<T>::at(w[k], e) + Vec<T>::at(q[k], e);
-                w[k] = pack_row<T>(v);
-                store_row<T>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V, a.streaming);
+                w[k] = settle_row<T, LPR == 8, STREAM>(pack_row<T>(v), c0 + k * LPR * V, cols);
+                put_row<T, STREAM>(h + c0 + k * LPR * V, w[k], cols - c0 - k * LPR * V);
             }
+        }
+        else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) w[k] = settle_row<T, LPR == 8, STREAM>(w[k], c0 + k * LPR * V, cols);
         }
         float y[NV][V], sum = 0.0f;
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, cols - c0 - k * LPR * V, y[k]);
+            load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, cols, y[k]);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float h = Vec<T>::at(w[k], e);
@@ -101,8 +106,8 @@ rmsnorm_rows(NormArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) y[k][e] *= rstd;
             const int64_t p = id * a.cols + c;
-            if (a.y) store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left, a.streaming);
-            store_codes<T>(a.codes + p, encode_values<V, MODE>(y[k], rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
+            if (a.y) put_row<T, STREAM>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
+            store_row_codes<T>(a.codes + p, encode_values<V, MODE>(y[k], rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
         }
     }
 }
@@ -124,9 +129,9 @@ rmsnorm_long(NormArgs a)
         uint32_t m = 0;
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.cols - c);
-            u32x4 w = load_row<T>(x + c, left);
+            u32x4 w = load_row<T>(x, (int)c, (int)a.cols);
             if (r) {
-                const u32x4 q = load_row<T>(r + c, left);
+                const u32x4 q = load_row<T>(r, (int)c, (int)a.cols);
                 float v[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = Vec<T>::at(w, e) + Vec<T>::at(q, e);
@@ -134,7 +139,7 @@ rmsnorm_long(NormArgs a)
                 store_row<T>(h + c, w, left);
             }
             float y[V];
-            load_weight<V>(a.w, a.w_bf16, c, left, y);
+            load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, y);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float v = Vec<T>::at(w, e);
@@ -153,14 +158,14 @@ rmsnorm_long(NormArgs a)
         const T* src = h ? h : x;                            // a thread's own stores where there is a residual
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.cols - c);
-            const u32x4 w = load_row<T>(src + c, left);
+            const u32x4 w = load_row<T>(src, (int)c, (int)a.cols);
             float y[V];
-            load_weight<V>(a.w, a.w_bf16, c, left, y);
+            load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, y);
 #pragma unroll
             for (int e = 0; e < V; ++e) y[e] = (Vec<T>::at(w, e) * y[e]) * rstd;
             const int64_t p = id * a.cols + c;
             if (a.y) store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y), left);
-            store_codes<T>(a.codes + p, encode_values<V, MODE>(y, rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
+            store_row_codes<T>(a.codes + p, encode_values<V, MODE>(y, rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
         }
     }
 }
@@ -171,7 +176,6 @@ struct NormGradArgs {
     const float* rstd;
     const void* w; int w_bf16;
     void* dx;
-    int streaming;                                     // dy, h and r are read by streaming loads (host)
     float* partial;                                    // [gridDim.x][cols] shares of dw, or null
     float* dw;
     int64_t batch, rows, cols;
@@ -180,7 +184,8 @@ struct NormGradArgs {
 
 // A thread's next row is on its way while it works on the current one; workgroups of 1024 threads, whose threads have 128 registers, do without,
 // and fetch the weights anew for every row.
-template <typename T, int LPR, int NV> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
+// STREAM: dy, h and r are read past the caches (host).
+template <typename T, int LPR, int NV, bool STREAM> __global__ void __launch_bounds__(LPR > 256 ? LPR : 256)
 rmsnorm_grad_rows(NormGradArgs a)
 {
     constexpr int V = Vec<T>::V, THREADS = LPR > 256 ? LPR : 256, RPB = THREADS / LPR;
@@ -192,7 +197,7 @@ rmsnorm_grad_rows(NormGradArgs a)
     float weight[NV][V], dw[NV][V];
     auto load_weights = [&]() {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, (int)a.cols - c0 - k * LPR * V, weight[k]);
+        for (int k = 0; k < NV; ++k) load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, (int)a.cols, weight[k]);
     };
     if constexpr (AHEAD) load_weights();
 #pragma unroll
@@ -210,10 +215,10 @@ rmsnorm_grad_rows(NormGradArgs a)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * LPR * V;
-            r.g[k] = load_row<T>(dy + c, cols - c, a.streaming);
-            r.w[k] = load_row<T>(h + c, cols - c, a.streaming);
+            r.g[k] = fetch_row<T, LPR == 8, STREAM>(dy, c, cols);
+            r.w[k] = fetch_row<T, LPR == 8, STREAM>(h, c, cols);
             r.q[k] = u32x4{0u, 0u, 0u, 0u};
-            if (a.r) r.q[k] = load_row<T>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row + c, cols - c, a.streaming);
+            if (a.r) r.q[k] = fetch_row<T, LPR == 8, STREAM>(static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row, c, cols);
         }
         r.rstd = live ? a.rstd[id] : 0.0f;
     };
@@ -226,6 +231,11 @@ rmsnorm_grad_rows(NormGradArgs a)
         Row next;
         if constexpr (AHEAD) { if ((blk + gridDim.x) * RPB < total) fetch(blk + gridDim.x, next); }
         else { fetch(blk, row); load_weights(); }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = c0 + k * LPR * V;
+            row.g[k] = settle_row<T, LPR == 8, STREAM>(row.g[k], c, cols); row.w[k] = settle_row<T, LPR == 8, STREAM>(row.w[k], c, cols); row.q[k] = settle_row<T, LPR == 8, STREAM>(row.q[k], c, cols);
+        }
         const float rstd = row.rstd;
         float sum = 0.0f;
         uint32_t none = 0;
@@ -296,9 +306,9 @@ rmsnorm_grad_long(NormGradArgs a)
         uint32_t none = 0;
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.cols - c);
-            const u32x4 g = load_row<T>(dy + c, left), w = load_row<T>(h + c, left);
+            const u32x4 g = load_row<T>(dy, (int)c, (int)a.cols), w = load_row<T>(h, (int)c, (int)a.cols);
             float weight[V];
-            load_weight<V>(a.w, a.w_bf16, c, left, weight);
+            load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, weight);
 #pragma unroll
             for (int e = 0; e < V; ++e) sum = fmaf(Vec<T>::at(g, e) * weight[e], Vec<T>::at(w, e) * rstd, sum);
         }
@@ -306,10 +316,10 @@ rmsnorm_grad_long(NormGradArgs a)
         const float mean = sum / (float)a.cols;
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.cols - c);
-            const u32x4 g = load_row<T>(dy + c, left), w = load_row<T>(h + c, left);
-            const u32x4 q = r ? load_row<T>(r + c, left) : u32x4{0u, 0u, 0u, 0u};
+            const u32x4 g = load_row<T>(dy, (int)c, (int)a.cols), w = load_row<T>(h, (int)c, (int)a.cols);
+            const u32x4 q = r ? load_row<T>(r, (int)c, (int)a.cols) : u32x4{0u, 0u, 0u, 0u};
             float weight[V], v[V];
-            load_weight<V>(a.w, a.w_bf16, c, left, weight);
+            load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, weight);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float n = Vec<T>::at(w, e) * rstd;
@@ -330,8 +340,8 @@ rmsnorm_grad_columns(NormGradArgs a)                   // grid (columns, shares)
     float dw[V] = {};
     for (int64_t id = blockIdx.y; id < total; id += gridDim.y) {
         const int64_t b = a.batch > 1 ? id / a.rows : 0, i = id - b * a.rows;
-        const u32x4 g = load_row<T>(static_cast<const T*>(a.dy) + b * a.dy_batch + i * a.dy_row + c, left);
-        const u32x4 w = load_row<T>(static_cast<const T*>(a.h) + b * a.h_batch + i * a.h_row + c, left);
+        const u32x4 g = load_row<T>(static_cast<const T*>(a.dy) + b * a.dy_batch + i * a.dy_row, (int)c, (int)a.cols);
+        const u32x4 w = load_row<T>(static_cast<const T*>(a.h) + b * a.h_batch + i * a.h_row, (int)c, (int)a.cols);
         const float rstd = a.rstd[id];
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[e] = fmaf(Vec<T>::at(g, e), Vec<T>::at(w, e) * rstd, dw[e]);
@@ -386,17 +396,20 @@ int64_t shares_of(const qmm_tensor* t)
     return blocks <= 4 ? 1 : std::min(blocks, most);
 }
 
-template <typename T, int MODE> qmm_status launch_norm(const NormArgs& a, hipStream_t s)
+template <typename T, int MODE> qmm_status launch_norm(const NormArgs& a, bool stream, hipStream_t s)
 {
     const int64_t total = a.batch * a.rows;
     if (a.cols > kRowElements) rmsnorm_long<T, MODE><<<row_blocks(total, 1), kRowLanes, 0, s>>>(a);
     else for_row_size<T>(a.cols, [&](auto lpr, auto nv) {
         constexpr int threads = lpr.value > 256 ? lpr.value : 256;
-        rmsnorm_rows<T, MODE, lpr.value, nv.value><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a);
+        if constexpr (lpr.value >= kWave) {
+            if (stream) { rmsnorm_rows<T, MODE, lpr.value, nv.value, true><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a); return; }
+        }
+        rmsnorm_rows<T, MODE, lpr.value, nv.value, false><<<row_blocks(total, threads / lpr.value), threads, 0, s>>>(a);
     });
     return launch_status();
 }
-template <typename T> qmm_status launch_norm_grad(NormGradArgs& a, hipStream_t s)
+template <typename T> qmm_status launch_norm_grad(NormGradArgs& a, bool stream, hipStream_t s)
 {
     const int64_t total = a.batch * a.rows;
     if (a.cols > kRowElements) {
@@ -409,7 +422,10 @@ template <typename T> qmm_status launch_norm_grad(NormGradArgs& a, hipStream_t s
     } else {
         for_row_size<T>(a.cols, [&](auto lpr, auto nv) {
             constexpr int threads = lpr.value > 256 ? lpr.value : 256;
-            rmsnorm_grad_rows<T, lpr.value, nv.value><<<(unsigned)a.shares, threads, 0, s>>>(a);
+            if constexpr (lpr.value >= kWave) {
+                if (stream) { rmsnorm_grad_rows<T, lpr.value, nv.value, true><<<(unsigned)a.shares, threads, 0, s>>>(a); return; }
+            }
+            rmsnorm_grad_rows<T, lpr.value, nv.value, false><<<(unsigned)a.shares, threads, 0, s>>>(a);
         });
     }
     if (a.partial && a.partial != a.dw) {
@@ -460,16 +476,14 @@ extern "C" qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor
     a.batch = x->batch; a.rows = x->rows; a.cols = x->cols;
     a.seed = seed; a.offset = offset; a.qmax = host_qmax(fmt); a.fmt = fmt;
     if (a.cols == 0) a.r = nullptr;
-    // h is wanted by the next addition to the residual stream, y by the backward pass: from where they would fill the caches between here and there
-    // they go past them, the codes, which the next product reads, do not (bfloat16 16384 x 4096 with y 115 -> 108 us, 8192 x 8192 97 -> 90,
-    // binary32 16384 x 4096 168 -> 154; 16384 x 1024, 33 MB, 22.7 -> 22.2)
-    // Reading x and the residual by streaming loads as well: 108 -> 102 and 90 -> 86; 16384 x 1024 22.5 -> 25.1.
-    a.x_streaming = residual && streams(x) && streams(residual);
-    a.streaming = a.batch * a.rows * a.cols * (x->dtype == QMM_DT_BF16 ? 2 : 4) >= (int64_t)64 << 20;
+    // The old residual stream is not read again, h is wanted by the next addition to it, y by the backward pass: where they are large they would fill the
+    // caches for nothing and go past them; the codes, which the next product reads, do not (bfloat16 16384 x 4096 with y 115 -> 102 us, 8192 x 8192 97 -> 86;
+    // 16384 x 1024, 33 MB, 22.5 -> 25.1).
+    const bool streaming = residual && streams(x) && streams(residual) && aligned16(h_out) && aligned16(y_out);
     hipStream_t s = as_stream(stream);
     if (x->dtype == QMM_DT_BF16)
-        return mode == QMM_ROUND_RTNE ? launch_norm<uint16_t, QMM_ROUND_RTNE>(a, s) : launch_norm<uint16_t, QMM_ROUND_STOCHASTIC>(a, s);
-    return mode == QMM_ROUND_RTNE ? launch_norm<float, QMM_ROUND_RTNE>(a, s) : launch_norm<float, QMM_ROUND_STOCHASTIC>(a, s);
+        return mode == QMM_ROUND_RTNE ? launch_norm<uint16_t, QMM_ROUND_RTNE>(a, streaming, s) : launch_norm<uint16_t, QMM_ROUND_STOCHASTIC>(a, streaming, s);
+    return mode == QMM_ROUND_RTNE ? launch_norm<float, QMM_ROUND_RTNE>(a, streaming, s) : launch_norm<float, QMM_ROUND_STOCHASTIC>(a, streaming, s);
 }
 
 extern "C" size_t qmm_rmsnorm_backward_workspace_size(const qmm_tensor* dy)
@@ -524,6 +538,6 @@ extern "C" qmm_status qmm_rmsnorm_backward(const qmm_tensor* dy, const qmm_tenso
     a.h = h->data; a.h_batch = h->batch_stride; a.h_row = h->row_stride;
     if (dresidual) { a.r = dresidual->data; a.r_batch = dresidual->batch_stride; a.r_row = dresidual->row_stride; }
     a.rstd = rstd; a.w = weight; a.w_bf16 = weight_dtype == QMM_DT_BF16; a.dx = dx_out;
-    a.streaming = streams(dy) && streams(h) && (!dresidual || streams(dresidual));       // (bfloat16 16384 x 4096 104 -> 95 us, 8192 x 8192 112 -> 108)
-    return dy->dtype == QMM_DT_BF16 ? launch_norm_grad<uint16_t>(a, s) : launch_norm_grad<float>(a, s);
+    const bool streaming = streams(dy) && streams(h) && (!dresidual || streams(dresidual));       // (bfloat16 16384 x 4096 104 -> 95 us, 8192 x 8192 112 -> 108)
+    return dy->dtype == QMM_DT_BF16 ? launch_norm_grad<uint16_t>(a, streaming, s) : launch_norm_grad<float>(a, streaming, s);
 }

@@ -8,11 +8,32 @@
 namespace qmm {
 namespace {
 
-template <typename T> QMM_DEV u32x4 load_row(const T* p, int left)          // V elements, zeros from `left` on
+// The vector of elements c .. c + V - 1 of a row of `cols`, zeros from there on; c a multiple of V.  In two steps, so that all of a row's loads are on their
+// way before the first is waited for: fetch_row takes a row's last elements with the vector that ends there, settle_row shifts that one.  (One by one, each
+// behind a branch and a wait, they were what a row of odd length took: bfloat16 8969 x 1491, the norm's backward pass 72 us against 28 of 1488 columns;
+// shifted where they were loaded 50.)  SHORT: rows of less than a vector are possible.  STREAM: a large tensor of whole lines that is not read again; its
+// lines are the first to leave the caches, else they take the place of what is still wanted.  (A constant of the kernel: chosen by a branch, the two loads
+// were made one ordinary one, or with what kept them apart 133 us where the gated gradients of 16384 x 4096 take 119.)
+template <typename T, bool SHORT = true, bool STREAM = false> QMM_DEV u32x4 fetch_row(const T* row, int c, int cols)
 {
-    if (left >= Vec<T>::V) return *reinterpret_cast<const u32x4_any*>(p);
-    return left > 0 ? Vec<T>::partial_load(p, left) : u32x4{0u, 0u, 0u, 0u};
+    constexpr int V = Vec<T>::V;
+    if (c >= cols) return u32x4{0u, 0u, 0u, 0u};
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + c));
+    if (SHORT && cols < V) return Vec<T>::partial_load(row, cols);
+    return *reinterpret_cast<const u32x4_any*>(row + min(c, cols - V));
 }
+template <typename T, bool SHORT = true, bool STREAM = false> QMM_DEV u32x4 settle_row(u32x4 w, int c, int cols)
+{
+    constexpr int V = Vec<T>::V;
+    if (!STREAM && c + V > cols && c < cols && (!SHORT || cols >= V)) {
+        const uint32_t away = (uint32_t)(c + V - cols) * sizeof(T);      // bytes of the elements before c
+        if (away & 8u) w = u32x4{w[2], w[3], 0u, 0u};
+        if (away & 4u) w = u32x4{w[1], w[2], w[3], 0u};
+        if constexpr (sizeof(T) == 2) { if (away & 2u) w = u32x4{(w[0] >> 16) | (w[1] << 16), (w[1] >> 16) | (w[2] << 16), (w[2] >> 16) | (w[3] << 16), w[3] >> 16}; }
+    }
+    return w;
+}
+template <typename T> QMM_DEV u32x4 load_row(const T* row, int c, int cols) { return settle_row<T>(fetch_row<T>(row, c, cols), c, cols); }
 // binary32 values -> a vector of the tensor's type, rounded to nearest even
 template <typename T> QMM_DEV u32x4 pack_row(const float* v)
 {
@@ -31,54 +52,50 @@ template <typename T> QMM_DEV u32x4 pack_row(const float* v)
 template <typename T> QMM_DEV void store_row(T* p, const u32x4& w, int left)
 {
     if (left >= Vec<T>::V) { *reinterpret_cast<u32x4_any*>(p) = w; return; }
-#pragma unroll
-    for (int e = 0; e < Vec<T>::V; ++e)
-        if (e < left) {
-            if constexpr (sizeof(T) == 4) p[e] = __uint_as_float(w[e]);
-            else p[e] = (T)(w[e >> 1] >> (16 * (e & 1)));
-        }
+    if (left > 0) store_bytes<16>(reinterpret_cast<uint8_t*>(p), w, left * (int)sizeof(T));
 }
-// The same of a large tensor that is not read again: streamed, its lines are the first to leave the caches, else they take the place of what is still wanted.
-template <typename T> QMM_DEV u32x4 load_row(const T* p, int left, int streaming)
+// The same of a vector's codes.
+template <typename T> QMM_DEV void store_row_codes(uint8_t* p, u32x2 c, int left)
 {
-    if (streaming && left >= Vec<T>::V) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-    return load_row<T>(p, left);
+    if (left >= Vec<T>::V) store_codes<T>(p, c, left);
+    else if (left > 0) store_bytes<8>(p, u32x4{c[0], c[1], 0u, 0u}, left);
 }
-// A vector's store, past the caches for outputs that are wanted again much later or do not fit them; `p` on a 16-byte boundary, or an ordinary one.
-template <typename T> QMM_DEV void store_row(T* p, const u32x4& w, int left, int streaming)
+// A vector's store, past the caches (STREAM; 16-byte boundaries) for outputs that are wanted again much later or do not fit them.
+template <typename T, bool STREAM> QMM_DEV void put_row(T* p, const u32x4& w, int left)
 {
-    if (streaming && left >= Vec<T>::V && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+    if constexpr (STREAM) { if (left > 0) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p)); }
     else store_row<T>(p, w, left);
 }
 // V elements of a vector of either type (the norm's weights), ones where there is none
-template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int left, float (&out)[V])
+template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int cols, float (&out)[V])
 {
 #pragma unroll
     for (int e = 0; e < V; ++e) out[e] = 1.0f;
-    if (!w || left <= 0) return;
-    if (bf16) {
-        const uint16_t* p = static_cast<const uint16_t*>(w) + c;
-        if constexpr (V == 8) {
-            const u32x4 q = load_row<uint16_t>(p, left);
-#pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = Vec<uint16_t>::at(q, e);
-        } else if (left >= V) {
-            typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-            const u32x2_any q = *reinterpret_cast<const u32x2_any*>(p);
-#pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = __uint_as_float((e & 1) ? (q[e >> 1] & 0xFFFF0000u) : (q[e >> 1] << 16));
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) if (e < left) out[e] = bf16_bits_to_f32(p[e]);
-        }
-    } else {
-        const float* p = static_cast<const float*>(w) + c;
+    if (!w || c >= cols) return;
+    if (!bf16) {
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) {
-            const u32x4 r = load_row<float>(p + 4 * q, left - 4 * q);
+            const u32x4 r = load_row<float>(static_cast<const float*>(w), c + 4 * q, cols);
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[4 * q + e] = __uint_as_float(r[e]);
         }
+    } else if constexpr (V == 8) {
+        const u32x4 q = load_row<uint16_t>(static_cast<const uint16_t*>(w), c, cols);
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = Vec<uint16_t>::at(q, e);
+    } else {
+        typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+        const uint16_t* p = static_cast<const uint16_t*>(w) + c;
+        const int left = cols - c;
+        uint64_t q = 0;
+        if (left >= V) q = __builtin_bit_cast(uint64_t, *reinterpret_cast<const u32x2_any*>(p));
+        else if (c > 0) q = __builtin_bit_cast(uint64_t, *reinterpret_cast<const u32x2_any*>(p - (V - left))) >> (16 * (V - left));
+        else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) if (e < left) q |= (uint64_t)p[e] << (16 * e);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = bf16_bits_to_f32((uint32_t)(q >> (16 * e)) & 0xFFFFu);
     }
 }
 
