@@ -55,6 +55,9 @@ rmsnorm_rows(NormArgs a)
         const int cols = live ? (int)a.cols : 0;
         const T* x = static_cast<const T*>(a.x) + b * a.x_batch + i * a.x_row;
         u32x4 w[NV];
+        Weights weight[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) weight[k] = fetch_weights<V>(a.w, a.w_bf16, c0 + k * LPR * V, cols);
 #pragma unroll
         for (int k = 0; k < NV; ++k) w[k] = fetch_row<T, LPR == 8, STREAM>(x, c0 + k * LPR * V, cols);
         if (a.r) {
@@ -81,7 +84,7 @@ rmsnorm_rows(NormArgs a)
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_weight<V>(a.w, a.w_bf16, c0 + k * LPR * V, cols, y[k]);
+            weight_values<V>(weight[k], a.w, a.w_bf16, c0 + k * LPR * V, cols, y[k]);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float h = Vec<T>::at(w[k], e);

@@ -66,37 +66,56 @@ template <typename T, bool STREAM> QMM_DEV void put_row(T* p, const u32x4& w, in
     if constexpr (STREAM) { if (left > 0) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p)); }
     else store_row<T>(p, w, left);
 }
-// V elements of a vector of either type (the norm's weights), ones where there is none
-template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int cols, float (&out)[V])
+// V of the norm's weights, of either type, ones where there is none: as they come from memory (so that they are requested in front of what is waited for
+// first), and as values.
+struct Weights { u32x4 w[2]; };
+template <int V> QMM_DEV Weights fetch_weights(const void* w, int bf16, int c, int cols)
 {
-#pragma unroll
-    for (int e = 0; e < V; ++e) out[e] = 1.0f;
-    if (!w || c >= cols) return;
+    Weights r{};
+    if (!w || c >= cols) return r;
     if (!bf16) {
 #pragma unroll
-        for (int q = 0; q < V / 4; ++q) {
-            const u32x4 r = load_row<float>(static_cast<const float*>(w), c + 4 * q, cols);
+        for (int q = 0; q < V / 4; ++q) r.w[q] = fetch_row<float>(static_cast<const float*>(w), c + 4 * q, cols);
+    } else if constexpr (V == 8) r.w[0] = fetch_row<uint16_t>(static_cast<const uint16_t*>(w), c, cols);
+    else {
+        typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+        const uint16_t* p = static_cast<const uint16_t*>(w);
+        if (cols >= V) {
+            const u32x2_any q = *reinterpret_cast<const u32x2_any*>(p + min(c, cols - V));
+            r.w[0][0] = q[0]; r.w[0][1] = q[1];
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[4 * q + e] = __uint_as_float(r[e]);
+            for (int e = 0; e < V; ++e) if (e < cols) r.w[0][e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        }
+    }
+    return r;
+}
+template <int V> QMM_DEV void weight_values(const Weights& r, const void* w, int bf16, int c, int cols, float (&out)[V])
+{
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = 1.0f;
+    } else if (!bf16) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            const u32x4 v = settle_row<float>(r.w[q], c + 4 * q, cols);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[4 * q + e] = __uint_as_float(v[e]);
         }
     } else if constexpr (V == 8) {
-        const u32x4 q = load_row<uint16_t>(static_cast<const uint16_t*>(w), c, cols);
+        const u32x4 v = settle_row<uint16_t>(r.w[0], c, cols);
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = Vec<uint16_t>::at(q, e);
+        for (int e = 0; e < V; ++e) out[e] = Vec<uint16_t>::at(v, e);
     } else {
-        typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-        const uint16_t* p = static_cast<const uint16_t*>(w) + c;
-        const int left = cols - c;
-        uint64_t q = 0;
-        if (left >= V) q = __builtin_bit_cast(uint64_t, *reinterpret_cast<const u32x2_any*>(p));
-        else if (c > 0) q = __builtin_bit_cast(uint64_t, *reinterpret_cast<const u32x2_any*>(p - (V - left))) >> (16 * (V - left));
-        else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) if (e < left) q |= (uint64_t)p[e] << (16 * e);
-        }
+        uint64_t q = r.w[0][0] | (uint64_t)r.w[0][1] << 32;
+        if (c + V > cols && c < cols && cols >= V) q >>= 16 * (c + V - cols);
 #pragma unroll
         for (int e = 0; e < V; ++e) out[e] = bf16_bits_to_f32((uint32_t)(q >> (16 * e)) & 0xFFFFu);
     }
+}
+template <int V> QMM_DEV void load_weight(const void* w, int bf16, int c, int cols, float (&out)[V])
+{
+    weight_values<V>(fetch_weights<V>(w, bf16, c, cols), w, bf16, c, cols, out);
 }
 
 // Sums and maxima over the LPR lanes that hold a row: within a wavefront by a butterfly, above 64 lanes over the workgroup (then
