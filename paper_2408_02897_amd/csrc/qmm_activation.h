@@ -8,6 +8,17 @@ namespace qmm {
 // last place; above 88.7 infinity, below -87.3 zero.
 QMM_DEV float exp_f32(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 QMM_DEV float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-x)); }
+// The same to 5 * 2^-24 relative for |x| < 80, as near as the operations around it round: what the product x log2(e) lost goes into the power to first
+// order, and the reciprocal takes a Newton step.  Beyond, and for what is not finite, logistic().  Gradients take it: their codes are compared with those of
+// values that round once, and one that falls to the other side of a tie is off by a whole step
+// (gated gradients of bfloat16 16384 x 4096: 122 us, with logistic() 119).
+QMM_DEV float logistic_exact(float x)
+{
+    const float t = x * -1.44269504f, lost = fmaf(t, 1.90465421e-9f, fmaf(t, -0.693147182f, -x));      // -x - t ln 2
+    const float p = __builtin_amdgcn_exp2f(t), d = 1.0f + p;
+    const float r = __builtin_amdgcn_rcpf(d), d2 = fmaf(p, lost, d);
+    return fabsf(x) < 80.0f ? fmaf(r, fmaf(-d2, r, 1.0f), r) : r;
+}
 
 // Phi(g), the normal distribution function: with z = |g|, Phi(-z) = exp(-z^2 / 2) q(z) where q(z) = erfcx(z / sqrt 2) / 2 falls slowly, like
 // 1 / z.  q as a polynomial of degree nine without constant term in t = 1 / (1 + 0.35 z), fitted over 0 <= z <= 15 for the least
@@ -39,7 +50,7 @@ template <int ACT> QMM_DEV float activate(float g)
 template <int ACT> QMM_DEV void activate_slope(float g, float& value, float& slope)
 {
     if constexpr (ACT == QMM_ACT_SILU) {
-        const float s = logistic(g);
+        const float s = logistic_exact(g);
         value = g * s;
         slope = s * fmaf(g, 1.0f - s, 1.0f);
     } else {

@@ -11,7 +11,7 @@
 // A thread keeps its columns' share of dw in registers over all rows of its workgroup; the workgroups' shares are added by a second
 // kernel in a fixed order, so dw does not depend on timing.
 // All of it is bound by memory traffic.  bfloat16 16384 x 4096, back to back on changing tensors: forward with residual, h and y (604 MB) 100 us, 6.0 TB/s;
-// backward with a residual's gradient (537 MB) 95 us, 5 of them the fold of dw, 5.7 TB/s; a plain copy of 1 GB runs at 6.0.  One row of 4096: 4 us,
+// backward with a residual's gradient (537 MB) 91 us, 5 of them the fold of dw, 5.9 TB/s; a plain copy of 1 GB runs at 6.0.  One row of 4096: 4 us,
 // a launch and two trips to memory and back.
 #include <type_traits>
 #include "qmm_rows.h"

@@ -10,8 +10,8 @@ namespace {
 
 // The vector of elements c .. c + V - 1 of a row of `cols`, zeros from there on; c a multiple of V.  In two steps, so that all of a row's loads are on their
 // way before the first is waited for: fetch_row takes a row's last elements with the vector that ends there, settle_row shifts that one.  (One by one, each
-// behind a branch and a wait, they were what a row of odd length took: bfloat16 8969 x 1491, the norm's backward pass 72 us against 28 of 1488 columns;
-// shifted where they were loaded 50.)  SHORT: rows of less than a vector are possible.  STREAM: a large tensor of whole lines that is not read again; its
+// behind a branch and a wait, they were what a row of odd length took: bfloat16 8969 x 1491, the norm's backward pass 70 us against 28 of 1488 columns;
+// shifted where they were loaded 50, now 30 and 26.)  SHORT: rows of less than a vector are possible.  STREAM: a large tensor of whole lines that is not read again; its
 // lines are the first to leave the caches, else they take the place of what is still wanted.  (A constant of the kernel: chosen by a branch, the two loads
 // were made one ordinary one, or with what kept them apart 133 us where the gated gradients of 16384 x 4096 take 119.)
 template <typename T, bool SHORT = true, bool STREAM = false> QMM_DEV u32x4 fetch_row(const T* row, int c, int cols)
@@ -67,7 +67,7 @@ template <typename T, bool STREAM> QMM_DEV void put_row(T* p, const u32x4& w, in
     else store_row<T>(p, w, left);
 }
 // V of the norm's weights, of either type, ones where there is none: as they come from memory (so that they are requested in front of what is waited for
-// first), and as values.
+// first: the norm of bfloat16 16384 x 4096 112 -> 107 us), and as values.
 struct Weights { u32x4 w[2]; };
 template <int V> QMM_DEV Weights fetch_weights(const void* w, int bf16, int c, int cols)
 {

@@ -545,3 +545,16 @@ def test_calls_on_several_streams():
     for k, w in enumerate(want):
         for g in got[k]:
             assert all(R.same_bits(g[n], w[n]) for n in w)
+
+
+def test_logistic_keeps_its_accuracy_in_the_tail():
+    # dh = 1 and u = 0: du = g s(g) alone.  Roundings: the power by an instruction of 2^-23 and one correction (3 * 2^-24 together, times
+    # 1 - s <= 1), 1 + e^-g, the last step of the reciprocal, g s, dh times it (2^-24 each), and 2^-24 for what is of second order: 8 * 2^-24.
+    g = torch.cat([torch.linspace(-79.9, 79.9, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30])])
+    gu = torch.cat([g, torch.zeros_like(g)]).unsqueeze(0)
+    got = qmm.gated_backward(torch.ones(1, g.numel(), device=DEV), gu.to(DEV), qmm.SILU, want_codes=False, want_dgu=True).dgu.cpu()[0, g.numel():].double()
+    want = g.double() * torch.sigmoid(g.double())
+    assert (got - want).abs().le(8 * 2.0 ** -24 * want.abs()).all()
+    far = torch.tensor([[float("inf"), 1e30, 100.0, -100.0, -1e30]])
+    got = qmm.gated_backward(torch.ones(1, 5, device=DEV), torch.cat([far, torch.zeros(1, 5)], 1).to(DEV), qmm.SILU, want_codes=False, want_dgu=True).dgu.cpu()[0, 5:]
+    assert got[:3].tolist() == far[0, :3].tolist() and got[3:].abs().le(1e-30).all()
