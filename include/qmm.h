@@ -310,8 +310,9 @@ qmm_status qmm_dequantize(const uint8_t* codes, int64_t batch, int64_t rows, int
  *   y_out         device, dense, x's type: y rounded once, or NULL.  rstd_out  device, batch * rows floats, or NULL.
  *   delta_out     device, batch * rows floats;  codes_out  device [batch][rows][cols]: an operand with per_channel = 1 and
  *                 batch_groups = batch.  Random bits of stochastic rounding as in qmm_quantize.
- * A row whose squares overflow binary32 has rstd 0, so y 0 and delta 1; a row with an inf or NaN has delta NaN and, in FP8, codes 0x7F.
- * A row of zeros has codes 0 and delta 1.  cols = 0: delta 1, rstd 1 / sqrt(eps).  Uses no workspace.
+ * A row whose squares overflow binary32 has rstd 0, so y 0 and delta 1, also where h_j * weight_j overflows; a row with an inf or NaN has delta NaN and,
+ * in FP8, codes 0x7F.  A row of zeros has y 0, codes 0 and delta 1, also with eps = 0, where its rstd is infinite and it has no gradient
+ * (qmm_rmsnorm_backward: NaN in its dx and in dw).  cols = 0: delta 1, rstd 1 / sqrt(eps).  Uses no workspace.
  * Other types, extents or axes: QMM_ERR_SHAPE / QMM_ERR_UNSUPPORTED / QMM_ERR_ENUM; a pointer off its element's boundary: QMM_ERR_ALIGN.
  */
 qmm_status qmm_rmsnorm_quantize(const qmm_tensor* x, const qmm_tensor* residual, const void* weight, qmm_dtype weight_dtype, float eps,

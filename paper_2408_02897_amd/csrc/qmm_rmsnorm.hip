@@ -37,6 +37,23 @@ QMM_DEV float rstd_of(float sum, int64_t cols, float eps)
     const float mean = cols > 0 ? sum / (float)cols : 0.0f;
     return 1.0f / sqrtf(mean + eps);
 }
+// What the products h w are multiplied by: 1 / rms.  A row without any (all zero: m, their largest magnitude, is 0) stays what it is where the root is zero
+// too (eps = 0), whose reciprocal times zero would be no number.
+QMM_DEV float factor_of(float rstd, uint32_t m) { return m == 0u ? 1.0f : rstd; }
+// A row whose squares are beyond binary32 has rstd 0 and is zero, unless an element is infinite.  Where h w is beyond binary32 as well, m = infinity does not tell
+// the two apart: the kernels then look at h and w again, each lane at the elements that it has read or written (elements c .. end - 1; one by one, so that
+// this costs the other rows nothing: with vectors, or h kept in registers for it, ten registers more).
+constexpr uint32_t kInfBits = 0x7F800000u;
+template <typename T> QMM_DEV bool finite_elements(const T* h, const void* w, int w_bf16, int c, int end)
+{
+    uint32_t m = 0;
+#pragma unroll 1
+    for (; c < end; ++c) {
+        m = max(m, mag_bits<T>(h[c]));
+        if (w) m = max(m, w_bf16 ? mag_bits<uint16_t>(static_cast<const uint16_t*>(w)[c]) : mag_bits<float>(static_cast<const float*>(w)[c]));
+    }
+    return m < kInfBits;
+}
 
 // Rows of up to kRowElements: LPR lanes hold one, NV vectors a lane.
 // STREAM: x and r are read, h and y written past the caches (host).
@@ -96,7 +113,23 @@ rmsnorm_rows(NormArgs a)
         RowReduce<LPR>::run(sum, m, sh, turn);
         if (!live) continue;                                 // (LPR > 64: never, a workgroup's only row is live)
         const float rstd = rstd_of(sum, a.cols, a.eps);
-        const float d = delta_from_absmax_bits(mag_bits(__uint_as_float(m) * rstd), a.qmax);
+        if (rstd == 0.0f && m == kInfBits) {
+            bool finite = true;
+#pragma unroll 1
+            for (int k = 0; k < NV; ++k)
+                finite &= finite_elements<T>(a.r ? static_cast<const T*>(a.h) + id * a.cols : x, a.w, a.w_bf16, c0 + k * LPR * V, min(c0 + k * LPR * V + V, cols));
+            m = finite ? 0u : kInfBits;
+            if constexpr (LPR > kWave) __syncthreads();      // the words of the reduction above have been read
+            RowReduce<LPR>::run(sum, m, sh, turn);
+            if (m == 0u) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y[k][e] = 0.0f;
+            }
+        }
+        const float factor = factor_of(rstd, m);
+        const float d = delta_from_absmax_bits(mag_bits(__uint_as_float(m) * factor), a.qmax);
         if (threadIdx.x % LPR == 0) {
             a.delta[id] = d;
             if (a.rstd) a.rstd[id] = rstd;
@@ -107,7 +140,7 @@ rmsnorm_rows(NormArgs a)
             const int c = c0 + k * LPR * V, left = cols - c;
             if (left <= 0) continue;
 #pragma unroll
-            for (int e = 0; e < V; ++e) y[k][e] *= rstd;
+            for (int e = 0; e < V; ++e) y[k][e] *= factor;
             const int64_t p = id * a.cols + c;
             if (a.y) put_row<T, STREAM>(static_cast<T*>(a.y) + p, pack_row<T>(y[k]), left);
             store_row_codes<T>(a.codes + p, encode_values<V, MODE>(y[k], rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
@@ -152,20 +185,31 @@ rmsnorm_long(NormArgs a)
         }
         RowReduce<kRowLanes>::run(sum, m, sh, turn);
         const float rstd = rstd_of(sum, a.cols, a.eps);
-        const float d = delta_from_absmax_bits(mag_bits(__uint_as_float(m) * rstd), a.qmax);
+        const T* src = h ? h : x;                            // a thread's own stores where there is a residual
+        bool zero = false;
+        if (rstd == 0.0f && m == kInfBits) {
+            bool finite = true;
+            for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V)
+                finite &= finite_elements<T>(src, a.w, a.w_bf16, (int)c, (int)min(c + V, a.cols));
+            m = finite ? 0u : kInfBits;
+            __syncthreads();
+            RowReduce<kRowLanes>::run(sum, m, sh, turn);
+            zero = m == 0u;
+        }
+        const float factor = factor_of(rstd, m);
+        const float d = delta_from_absmax_bits(mag_bits(__uint_as_float(m) * factor), a.qmax);
         if (threadIdx.x == 0) {
             a.delta[id] = d;
             if (a.rstd) a.rstd[id] = rstd;
         }
         const float rho = 1.0f / d;
-        const T* src = h ? h : x;                            // a thread's own stores where there is a residual
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
             const int left = (int)min((int64_t)V, a.cols - c);
             const u32x4 w = load_row<T>(src, (int)c, (int)a.cols);
             float y[V];
             load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, y);
 #pragma unroll
-            for (int e = 0; e < V; ++e) y[e] = (Vec<T>::at(w, e) * y[e]) * rstd;
+            for (int e = 0; e < V; ++e) y[e] = zero ? 0.0f : (Vec<T>::at(w, e) * y[e]) * factor;
             const int64_t p = id * a.cols + c;
             if (a.y) store_row<T>(static_cast<T*>(a.y) + p, pack_row<T>(y), left);
             store_row_codes<T>(a.codes + p, encode_values<V, MODE>(y, rho, a.fmt, (uint64_t)p + a.offset, a.seed), left);
