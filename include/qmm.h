@@ -349,7 +349,8 @@ typedef enum { QMM_ACT_SILU = 0, QMM_ACT_GELU = 1 } qmm_activation;
  *              qmm_gated_backward; or NULL.
  *   workspace  qmm_gemm_gated_workspace_size() bytes, 16-byte aligned (0: may be NULL).  It is non-zero where M and F are small
  *              and K long: K is then split and the parts are added in a fixed order.
- * e^-g and Phi are evaluated in binary32 to a few units of the last place (relative to |g| 2^-23 where e^-g is far from 1).
+ * The activations are evaluated in binary32: act(g) is off by at most (1.3 |g| + 8) 2^-24 (SiLU, |g| <= 80) or (1.2 g^2 + 18) 2^-24 (GELU, |g| <= 12.5) of
+ * itself, the loss of the power's argument; further out, where act(g) nears the smallest normal value, to that.
  * A gate of -infinity gives NaN.  F up to 2^22, else QMM_ERR_UNSUPPORTED.  Other rules and errors as for qmm_gemm.
  */
 size_t qmm_gemm_gated_workspace_size(const qmm_operand* a, const qmm_operand* b, int64_t batch, int64_t M, int64_t F, int64_t K);

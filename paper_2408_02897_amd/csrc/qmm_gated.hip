@@ -3,7 +3,8 @@
 // for a token's whole row (g | u), as values for the weight gradient and, quantized with one step size per token (Eq. 1), as the
 // codes of the data gradient's operand.  A row is read once, its 2 F results stay in registers until their largest magnitude is known:
 // the codes are of the binary32 results, not of their bfloat16 roundings.
-// Bound by memory traffic: bfloat16 reads 6 bytes and writes 4 + 2 a pair; 16384 x 4096 (805 MB) 118 us, 6.8 TB/s, GELU's as SiLU's.
+// Bound by memory traffic: bfloat16 reads 6 bytes and writes 4 + 2 a pair; 16384 x 4096 (805 MB) 120 us, 6.7 TB/s; GELU's, whose vector work
+// comes near that time, 127.
 #include "qmm_activation.h"
 #include "qmm_rows.h"
 
@@ -27,7 +28,7 @@ template <typename T, int ACT> QMM_DEV void gated_grad(const u32x4& dh, const u3
     for (int e = 0; e < Vec<T>::V; ++e) {
         const float d = Vec<T>::at(dh, e);
         float value, slope;
-        activate_slope<ACT>(Vec<T>::at(g, e), value, slope);
+        activate_slope<ACT, sizeof(T) == 2>(Vec<T>::at(g, e), value, slope);
         dg[e] = (d * Vec<T>::at(u, e)) * slope;
         du[e] = d * value;
     }

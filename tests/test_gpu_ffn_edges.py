@@ -56,3 +56,53 @@ def test_norm_of_rows_without_a_root_mean_square(cols, dtype):
 def test_norm_without_columns_or_eps():
     e = qmm.rmsnorm_quantize(torch.empty((3, 0), device=DEV), None, qmm.E4M3, eps=0.0, want_rstd=True)
     assert torch.all(e.delta == 1) and torch.all(e.rstd == float("inf")) and e.codes.shape == (1, 3, 0)
+
+
+# ------------------------------------------------------------------------------------------------ activations far out
+# GELU: Phi(-z) = e^(-z^2/2) q(z).  In units of 2^-24, relative: q 12 (the fit 1.1, its evaluation 3.9, the argument's two roundings and reciprocal 3 times
+# |t q' / q| <= 2.3) at z = 0 and falling faster than the power's constants gain, 0.023 z^2 (12.5: 6.2 + 3.6); the power 2 by the instruction and 2 by its
+# correction, the product with q, that with g: 18.
+PHI = 18 * 2.0 ** -24
+
+
+def gates():
+    return torch.cat([torch.linspace(-12.5, 12.5, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30])])
+
+
+def gated_grad_of(g, u, kind):
+    """dg and du of dh = 1."""
+    gu = torch.cat([g, u]).unsqueeze(0)
+    v = qmm.gated_backward(torch.ones(1, g.numel(), device=DEV), gu.to(DEV), kind, want_codes=False, want_dgu=True).dgu.cpu()[0].double()
+    return v[:g.numel()], v[g.numel():]
+
+
+def test_gelu_keeps_its_accuracy_in_the_tail():
+    g = gates()
+    dg, du = gated_grad_of(g, torch.ones_like(g), qmm.GELU)
+    z = g.double()
+    phi, density = R.phi(z), torch.exp(-z * z / 2) * 0.3989422804014327
+    assert (du - z * phi).abs().le(PHI * (z * phi).abs()).all()
+    # the slope Phi + g phi(g): phi's power 4 and 3.6, its constant, a product; the sum's rounding
+    assert (dg - (phi + z * density)).abs().le(PHI * phi + 10 * 2.0 ** -24 * (z * density).abs() + 2.0 ** -24 * (phi + z * density).abs()).all()
+    far = torch.tensor([1e30, 3e38, 100.0, -100.0, -1e30, -3e38])
+    dg, du = gated_grad_of(far, torch.ones(6), qmm.GELU)
+    assert dg.tolist() == [1, 1, 1, 0, 0, 0] and du[:3].tolist() == far[:3].double().tolist() and torch.all(du[3:] == 0)
+    dg, du = gated_grad_of(torch.tensor([float("nan"), float("-inf")]), torch.ones(2), qmm.GELU)
+    assert torch.isnan(dg).all() and torch.isnan(du).all()
+
+
+@pytest.mark.parametrize("m", [1, 100])
+@pytest.mark.parametrize("kind", [qmm.SILU, qmm.GELU])
+def test_product_keeps_the_stated_accuracy_in_the_tail(kind, m):
+    # The header's bounds.  In units of 2^-24: the power's argument loses 1.22 of itself (the product with log2(e) and its constant; the square another 1), SiLU: the
+    # instruction 2, the sum 1, the reciprocal 2, the product 1; GELU: q 12, the instruction 2, three products.
+    g = torch.cat([gates()[:4000], torch.linspace(-80, 80, 4000) if kind == qmm.SILU else gates()[:4000]]).to(BF)
+    f = g.numel()
+    a, b = torch.zeros(m, 16, dtype=BF, device=DEV), torch.zeros(2 * f, 16, dtype=BF)
+    a[:, 0], b[:f, 0], b[f:, 0] = 1.0, g, 1.0
+    b = b.to(DEV)
+    h = qmm.gemm_gated((a, qmm.operand(a, qmm.BF16, is_codes=False)), (b, qmm.operand(b, qmm.BF16, is_codes=False)), kind, F32)[0].cpu().double()
+    z = g.double()
+    want = R.act(z, kind)[0]
+    off = (1.3 * z.abs() + 8 if kind == qmm.SILU else 1.2 * z * z + 18) * 2.0 ** -24
+    assert ((h - want).abs() <= off * want.abs()).all()
