@@ -11,13 +11,17 @@ QMM_DEV float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-x
 // The same to 5 * 2^-24 relative for |x| < 80, as near as the operations around it round: what the product x log2(e) lost goes into the power to first
 // order, and the reciprocal takes a Newton step.  Beyond, and for what is not finite, logistic().  Gradients take it: their codes are compared with those of
 // values that round once, and one that falls to the other side of a tie is off by a whole step
-// (gated gradients of bfloat16 16384 x 4096: 122 us, with logistic() 119).
-QMM_DEV float logistic_exact(float x)
+// (gated gradients of bfloat16 16384 x 4096: 122 us, with logistic() and 1 - s 118).
+// rest: 1 - s, for x >= 0 as e^-x s to 9 * 2^-24 relative (s being near 1, the subtraction loses up to all of it).
+QMM_DEV float logistic_exact(float x, float& rest)
 {
     const float t = x * -1.44269504f, lost = fmaf(t, 1.90465421e-9f, fmaf(t, -0.693147182f, -x));      // -x - t ln 2
     const float p = __builtin_amdgcn_exp2f(t), d = 1.0f + p;
     const float r = __builtin_amdgcn_rcpf(d), d2 = fmaf(p, lost, d);
-    return fabsf(x) < 80.0f ? fmaf(r, fmaf(-d2, r, 1.0f), r) : r;
+    const bool near = fabsf(x) < 80.0f;
+    const float s = near ? fmaf(r, fmaf(-d2, r, 1.0f), r) : r;
+    rest = near && x >= 0.0f ? fmaf(p, lost, p) * s : 1.0f - s;
+    return s;
 }
 
 // e^(-g^2 / 2) to 4 * 2^-24 relative and g^2 2^-29 from the constant, to zero from |g| = 16 on: what the product with log2(e) and (unless SQUARE: g has at most
@@ -62,9 +66,10 @@ template <int ACT> QMM_DEV float activate(float g)
 template <int ACT, bool SQUARE> QMM_DEV void activate_slope(float g, float& value, float& slope)
 {
     if constexpr (ACT == QMM_ACT_SILU) {
-        const float s = logistic_exact(g);
+        float rest;
+        const float s = logistic_exact(g, rest);
         value = g * s;
-        slope = s * fmaf(g, 1.0f - s, 1.0f);
+        slope = s * fmaf(g, rest, 1.0f);
     } else {
         const float e = exp_half_square<SQUARE>(g), p = normal_cdf(g, e);
         value = g * p;
