@@ -336,6 +336,29 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// Whether an operand reads what its tensor holds (_check_operand of qmm.py): the same memory, elements of its format, a step size for every row.
+bool holds(PyObject* pair, const at::Tensor& t, const qmm_operand& op, int64_t batch, int64_t rows)
+{
+    const bool bf16 = op.format == QMM_FMT_BF16;
+    if (op.data != t.data_ptr() || !t.is_contiguous() || (!bf16 && !op.is_codes) || t.element_size() != (bf16 ? 2 : 1)) return false;
+    static PyObject* const name = PyUnicode_InternFromString("_keep");
+    PyObject* keep = PyObject_GetAttr(PyTuple_GET_ITEM(pair, 1), name);
+    if (!keep) { PyErr_Clear(); return false; }
+    bool good = PyTuple_CheckExact(keep) && PyTuple_GET_SIZE(keep) == 2;
+    PyObject* d = good ? PyTuple_GET_ITEM(keep, 1) : nullptr;
+    if (good && d != Py_None) {
+        good = plain(d);
+        if (good) {
+            const at::Tensor& delta = THPVariable_Unpack(d);
+            const int64_t groups = std::min<int64_t>(op.gran.batch_groups, (batch - 1) / std::max(op.gran.batch_inner, 1) + 1);
+            good = here(delta) && delta.scalar_type() == at::kFloat && delta.is_contiguous() && op.delta == delta.data_ptr() &&
+                   delta.numel() >= std::max<int64_t>(groups, 0) * (op.gran.per_channel ? rows : 1);
+        }
+    }
+    Py_DECREF(keep);
+    return good;
+}
+
 // args: a, b, activation, out_dtype, want_gu -> (h, gu)
 PyObject* gemm_gated(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -349,7 +372,8 @@ PyObject* gemm_gated(PyObject*, PyObject* const* args, Py_ssize_t n)
     const int64_t d = ta->dim();
     if (!here(*ta) || !here(*tb) || (d != 2 && d != 3) || tb->dim() != d || (type != at::kBFloat16 && type != at::kFloat)) Py_RETURN_NONE;
     const int64_t batch = d == 3 ? ta->size(0) : 1, M = ta->size(d - 2), K = ta->size(d - 1), F = tb->size(d - 2) / 2;
-    if ((d == 3 && tb->size(0) != batch) || tb->size(d - 1) != K || tb->size(d - 2) % 2) Py_RETURN_NONE;
+    if ((d == 3 && tb->size(0) != batch) || tb->size(d - 1) != K || tb->size(d - 2) % 2 || !holds(args[0], *ta, oa, batch, M) ||
+        !holds(args[1], *tb, ob, batch, 2 * F)) Py_RETURN_NONE;
     at::Tensor h, gu, ws;
     qmm_status st;
     {

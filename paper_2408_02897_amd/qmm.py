@@ -476,9 +476,26 @@ def rmsnorm_backward(dy, h, rstd, weight, dresidual=None, want_dw=True, dx_out=N
     return dx, dw
 
 
+def _check_operand(t, op, batch, rows):
+    """An operand reads what its tensor holds: the same memory, elements of its format, a step size for every row of every group (of an operand made by
+    `operand` or quantized_operand, which know their tensors).  What the library refuses itself is left to it."""
+    if (op.data or 0) != t.data_ptr() or not t.is_contiguous():
+        raise ValueError("an operand of another tensor")
+    if (op.format == BF16 or op.is_codes) and t.element_size() != (2 if op.format == BF16 else 1):
+        raise ValueError(f"{t.dtype} in an operand of format {op.format}")
+    delta = getattr(op, "_keep", (None, None))[1]
+    if delta is None:
+        return
+    groups = min(op.gran.batch_groups, (batch - 1) // max(op.gran.batch_inner, 1) + 1)
+    need = max(groups, 0) * (rows if op.gran.per_channel else 1)
+    if delta.dtype != torch.float32 or not delta.is_contiguous() or delta.numel() < need or (op.delta or 0) != delta.data_ptr():
+        raise ValueError(f"{delta.numel()} step sizes of {delta.dtype}, not {need} of float32 side by side")
+    _on(t.device, delta)
+
+
 def gemm_gated(a, b, activation=SILU, out_dtype=torch.bfloat16, want_gu=False):
     """qmm_gemm_gated on two (data, Operand) pairs as `gemm` takes them, b = ([batch, 2 F, K], Operand) with the gate's rows first:
-    h [batch, M, F], or (h, gu [batch, M, 2 F]) when want_gu."""
+    h [batch, M, F], or (h, gu [batch, M, 2 F]) when want_gu.  An operand that describes more than its tensors hold: ValueError."""
     r = (_short or _host()).gemm_gated(a, b, activation, out_dtype, want_gu)
     if type(r) is int:
         _check(r, "qmm_gemm_gated")
@@ -493,6 +510,8 @@ def gemm_gated(a, b, activation=SILU, out_dtype=torch.bfloat16, want_gu=False):
     bt, m, k = sa
     assert len(sb) == 3 and sb[0] == bt and sb[2] == k and sb[1] % 2 == 0, "b is [batch, 2 F, K]"
     f = sb[1] // 2
+    _check_operand(ta, oa, bt, m)
+    _check_operand(tb, ob, bt, 2 * f)
     h = torch.empty((bt, m, f), dtype=out_dtype, device=dev)
     gu = torch.empty((bt, m, 2 * f), dtype=out_dtype, device=dev) if want_gu else None
     pa, pb = ctypes.byref(oa), ctypes.byref(ob)

@@ -133,3 +133,42 @@ def test_the_binding_refuses_what_the_library_cannot_see():
     op = qmm.operand(torch.zeros((4, 32), dtype=torch.uint8), qmm.E4M3, torch.ones(1))
     with pytest.raises(ValueError):
         qmm.gemm_gated((x, op), (x, op))
+
+
+def test_gated_product_refuses_operands_that_read_past_their_tensors(monkeypatch):
+    """Step sizes or elements that are not there: refused before the library is called (the kernels read what the descriptor says)."""
+    class Reached(Exception):
+        pass
+
+    class Library:
+        def __getattr__(self, name):
+            if "workspace" in name:
+                return lambda *_: 0
+            raise Reached(name)
+    monkeypatch.setattr(qmm, "_on", lambda device, *tensors: device)
+    monkeypatch.setattr(qmm, "lib", Library)
+    monkeypatch.setattr(qmm, "_short", qmm._NoShortPath)
+    codes = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    x, w = codes(4, 32), codes(20, 32)
+    op = lambda t, n, fmt=qmm.E4M3, **k: (t, qmm.operand(t, fmt, torch.ones(n), **k))
+    whole = op(x, 4, per_channel=True), op(w, 20, per_channel=True)
+    good = [whole, (op(x, 1), op(w, 1)), (op(x, 9, per_channel=True), op(w, 3)),
+            (op(codes(6, 4, 32), 3 * 4, per_channel=True, batch_groups=3), op(codes(6, 20, 32), 2, batch_groups=2, batch_inner=3)),
+            (op(codes(2, 4, 32), 4 * 2, per_channel=True, batch_groups=5), op(codes(2, 20, 32), 1, batch_groups=4, batch_inner=2))]
+    bf = [t.to(torch.bfloat16) for t in (x, w)]
+    good.append(tuple((t, qmm.operand(t, qmm.BF16, is_codes=False)) for t in bf))
+    raw = qmm.operand(x, qmm.E4M3, torch.ones(1))
+    good.append(((x, qmm.Operand(raw.data, raw.format, 1, raw.delta, raw.gran)), whole[1]))           # a descriptor of the caller's own
+    for a, b in good:
+        with pytest.raises(Reached):
+            qmm.gemm_gated(a, b)
+    bad = [(op(x, 3, per_channel=True), whole[1]), (whole[0], op(w, 10, per_channel=True)),             # the gate's step sizes only
+           (op(codes(6, 4, 32), 2 * 4, per_channel=True, batch_groups=3), op(codes(6, 20, 32), 1)),
+           (whole[0], (codes(22, 32), whole[1][1])), (op(codes(4, 16), 4, per_channel=True), (w[:, :16], whole[1][1])),     # the descriptor of another tensor
+           ((x, qmm.operand(x, qmm.E4M3, torch.ones(4, dtype=torch.float64))), whole[1]),
+           ((x, qmm.operand(x, qmm.E4M3, torch.ones(8)[::2], per_channel=True)), whole[1]),
+           tuple((t, qmm.operand(t, qmm.BF16, is_codes=False)) for t in (x, w)),                        # bytes as bfloat16
+           ((bf[0], qmm.operand(bf[0], qmm.E4M3, torch.ones(1))), whole[1])]
+    for a, b in bad:
+        with pytest.raises(ValueError):
+            qmm.gemm_gated(a, b)

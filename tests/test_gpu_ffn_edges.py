@@ -119,3 +119,18 @@ def test_silu_slope_keeps_its_accuracy():
     far = torch.tensor([1e30, 3e38, 100.0, -100.0, -1e30, -3e38])
     dg, _ = gated_grad_of(far, torch.ones(6), qmm.SILU)
     assert dg[:3].tolist() == [1, 1, 1] and dg[3:].abs().le(1e-30).all()
+
+
+# ------------------------------------------------------------------------------------------------ operands
+def test_gated_product_refuses_operands_that_read_past_their_tensors(monkeypatch):
+    x, w = torch.zeros((4, 32), dtype=torch.uint8, device=DEV), torch.zeros((20, 32), dtype=torch.uint8, device=DEV)
+    op = lambda t, n, **k: (t, qmm.operand(t, qmm.E4M3, torch.ones(n, device=DEV), **k))
+    a, b = op(x, 4, per_channel=True), op(w, 20, per_channel=True)
+    for short in (None, qmm._NoShortPath):
+        monkeypatch.setattr(qmm, "_short", short)
+        for good in ((a, b), (op(x, 1), b), (op(x, 7, per_channel=True), op(w, 2))):
+            assert torch.all(qmm.gemm_gated(*good) == 0)
+        for bad in ((op(x, 3, per_channel=True), b), (a, op(w, 10, per_channel=True)), (a, (torch.zeros_like(w), b[1])), (op(x.to(BF), 4, per_channel=True), b),
+                    (a, (w, qmm.operand(w, qmm.E4M3, torch.ones(20), per_channel=True)))):
+            with pytest.raises(ValueError):
+                qmm.gemm_gated(*bad)
