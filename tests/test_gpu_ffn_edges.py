@@ -121,6 +121,71 @@ def test_silu_slope_keeps_its_accuracy():
     assert dg[:3].tolist() == [1, 1, 1] and dg[3:].abs().le(1e-30).all()
 
 
+# ------------------------------------------------------------------------------------------------ backward passes of batches
+def apart(t, rows, cols):
+    """The same batch with `rows` rows between the matrices and `cols` elements between the rows, filled with NaN, off a 16-byte boundary."""
+    b, r, c = t.shape
+    big = torch.full((b * (r + rows) * (c + cols) + 1,), float("nan"), dtype=t.dtype, device=DEV)[1:].view(b, r + rows, c + cols)
+    v = big[:, :r, :c]
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,cols", [(7, 30), (11, 100), (401, 64), (5, 1000), (9, 4104), (3, 16400)])
+def test_norm_backward_of_batches(rows, cols, dtype):
+    dy, h, r = normal(1, 3, rows, cols, dtype=dtype, scale=0.01), normal(2, 3, rows, cols, dtype=dtype, scale=2.0), normal(3, 3, rows, cols, dtype=dtype, scale=0.01)
+    w = 1 + 0.3 * normal(4, cols)
+    rstd = R.norm(h, None, None, 1e-5)[2].float()
+    dx, dw, size, size_w = R.norm_grad(dy, h, rstd, w, r)
+    for args in ((dy.to(DEV), h.to(DEV), r.to(DEV)), (apart(dy, 2, 3), apart(h, 1, 0), apart(r, 0, 5))):
+        gx, gw = qmm.rmsnorm_backward(args[0], args[1], rstd.reshape(-1).to(DEV), w.to(DEV), dresidual=args[2])
+        assert gx.shape == dy.shape
+        assert ((gx.cpu().double() - dx).abs() <= SUM * size + R.rounding(dtype) * dx.abs()).all()
+        assert ((gw.cpu().double() - dw).abs() <= SUM * size_w).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,f", [(7, 30), (11, 100), (5, 1000), (9, 4104), (3, 16400)])
+def test_gated_backward_of_batches(rows, f, dtype):
+    dh, gu = normal(1, 3, rows, f, dtype=dtype), normal(2, 3, rows, 2 * f, dtype=dtype, scale=1.5)
+    g, u, d = gu[..., :f].double(), gu[..., f:].double(), dh.double()
+    for kind in (qmm.SILU, qmm.GELU):
+        value, slope = R.act(g, kind)
+        want = torch.cat([d * u * slope, d * value], -1)
+        # |g| <= 8 here: the terms of the slope, relative to 32 roundings each (the tests above)
+        terms = torch.cat([(d * u).abs() * (1 + g.abs()), (d * value).abs()], -1)
+        for args in ((dh.to(DEV), gu.to(DEV)), (apart(dh, 2, 3), apart(gu, 1, 5))):
+            got = qmm.gated_backward(*args, kind, qmm.E5M2, want_dgu=True)
+            assert got.dgu.shape == gu.shape and got.codes.shape == gu.shape
+            off = 32 * 2.0 ** -24 * terms
+            assert ((got.dgu.cpu().double() - want).abs() <= off + R.rounding(dtype) * (want.abs() + off)).all()
+            R.check_codes(got.codes, got.delta, want, qmm.E5M2, 2.0 ** -14)
+
+
+# ------------------------------------------------------------------------------------------------ large outputs over inputs
+def test_large_outputs_over_inputs():
+    """From 64 MB on rows are read and written past the caches: the same results where an output takes an input's memory."""
+    rows, cols = 8192, 4096
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x, r = (torch.randn((rows, cols), generator=g, device=DEV, dtype=BF) for _ in range(2))
+    w = torch.rand(cols, generator=g, device=DEV) + 0.5
+    n = qmm.rmsnorm_quantize(x, w, qmm.E4M3, residual=r, want_y=True, want_rstd=True)
+    for which in range(2):
+        t = [x.clone(), r.clone()]
+        m = qmm.rmsnorm_quantize(t[0], w, qmm.E4M3, residual=t[1], want_y=True, want_rstd=True, h_out=t[which])
+        assert m.h is t[which] and all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(n, m))
+    dx, dw = qmm.rmsnorm_backward(n.y, n.h, n.rstd, w, dresidual=r)
+    for which in range(3):
+        t = [n.y.clone(), n.h.clone(), r.clone()]
+        dx2, dw2 = qmm.rmsnorm_backward(t[0], t[1], n.rstd, w, dresidual=t[2], dx_out=t[which])
+        assert dx2 is t[which] and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    gu = torch.randn((rows, 2 * cols), generator=g, device=DEV, dtype=BF)
+    d = qmm.gated_backward(x, gu, qmm.SILU, qmm.E5M2, want_dgu=True)
+    e = qmm.gated_backward(x, gu, qmm.SILU, qmm.E5M2, dgu_out=gu)
+    assert e.dgu is gu and torch.equal(d.dgu, gu) and torch.equal(d.codes, e.codes) and torch.equal(d.delta, e.delta)
+
+
 # ------------------------------------------------------------------------------------------------ operands
 def test_gated_product_refuses_operands_that_read_past_their_tensors(monkeypatch):
     x, w = torch.zeros((4, 32), dtype=torch.uint8, device=DEV), torch.zeros((20, 32), dtype=torch.uint8, device=DEV)
