@@ -103,7 +103,6 @@ gated_grad_long(GatedGradArgs a)
         uint32_t m = 0;
         if (a.codes) {
             for (int64_t c = (int64_t)threadIdx.x * V; c < a.F; c += kRowLanes * V) {
-                const int left = (int)min((int64_t)V, a.F - c);
                 gated_grad<T, ACT>(load_row<T>(dh, (int)c, (int)a.F), load_row<T>(g, (int)c, (int)a.F), load_row<T>(g + a.F, (int)c, (int)a.F), dg, du);
 #pragma unroll
                 for (int e = 0; e < V; ++e) m = max(m, max(mag_bits(dg[e]), mag_bits(du[e])));

@@ -185,7 +185,7 @@ template <int T> QMM_DEV void store_bf16(uint16_t* dst, const float (&v)[T])
 
 constexpr int kGatedSlots = 3;                             // ring of gated_deep_kernel
 constexpr int kGatedFew = 64;                              // tokens up to which gated_few_kernel serves
-constexpr int64_t kGatedColumns = int64_t(1) << 22;          // F up to which 64 rows of (g | u) in binary32 lie within 32-bit offsets
+[[maybe_unused]] constexpr int64_t kGatedColumns = int64_t(1) << 22;          // F up to which 64 rows of (g | u) in binary32 lie within 32-bit offsets
 
 // Gated products.  The weights are the first operand: a lane of the matrix instructions then holds several rows of a block, i.e. columns of the
 // output, of one token.  Of a wavefront's blocks of 16 (32) weight rows every other one is of `up`, the one in front of it of

@@ -352,7 +352,6 @@ rmsnorm_grad_long(NormGradArgs a)
         float sum = 0.0f;
         uint32_t none = 0;
         for (int64_t c = (int64_t)threadIdx.x * V; c < a.cols; c += kRowLanes * V) {
-            const int left = (int)min((int64_t)V, a.cols - c);
             const u32x4 g = load_row<T>(dy, (int)c, (int)a.cols), w = load_row<T>(h, (int)c, (int)a.cols);
             float weight[V];
             load_weight<V>(a.w, a.w_bf16, (int)c, (int)a.cols, weight);
