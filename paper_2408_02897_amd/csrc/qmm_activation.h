@@ -8,25 +8,23 @@ namespace qmm {
 // last place; above 88.7 infinity, below -87.3 zero.
 QMM_DEV float exp_f32(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 QMM_DEV float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-x)); }
-// The same to 5 * 2^-24 relative for |x| < 80, as near as the operations around it round: what the product x log2(e) lost goes into the power to first
-// order, and the reciprocal takes a Newton step.  Beyond, and for what is not finite, logistic().  Gradients take it: their codes are compared with those of
-// values that round once, and one that falls to the other side of a tie is off by a whole step
-// (gated gradients of bfloat16 16384 x 4096: 122 us, with logistic() and 1 - s 118).
-// rest: 1 - s, for x >= 0 as e^-x s to 9 * 2^-24 relative (s being near 1, the subtraction loses up to all of it).
+// The same to 5 * 2^-24 relative for x > -87, as near as the operations around it round: what the product x log2(e) lost goes into the power to first
+// order, and the reciprocal takes a Newton step.  rest: 1 - s as e^-x s to 9 * 2^-24 relative (s being near 1, the subtraction loses up to all of it).  Below -88
+// s is zero, above 104 e^-x is.  Gradients take it: their codes are compared with those of values that round once, and one that falls to the other side of a
+// tie is off by a whole step (gated gradients of bfloat16 16384 x 4096: 120 us, with logistic() and 1 - s 119).
 QMM_DEV float logistic_exact(float x, float& rest)
 {
-    const float t = x * -1.44269504f, lost = fmaf(t, 1.90465421e-9f, fmaf(t, -0.693147182f, -x));      // -x - t ln 2
-    const float p = __builtin_amdgcn_exp2f(t), d = 1.0f + p;
-    const float r = __builtin_amdgcn_rcpf(d), d2 = fmaf(p, lost, d);
-    const bool near = fabsf(x) < 80.0f;
-    const float s = near ? fmaf(r, fmaf(-d2, r, 1.0f), r) : r;
-    rest = near && x >= 0.0f ? fmaf(p, lost, p) * s : 1.0f - s;
-    return s;
+    const float c = __builtin_amdgcn_fmed3f(x, -88.0f, 104.0f), t = c * -1.44269504f;
+    const float lost = fmaf(t, 1.90465421e-9f, fmaf(t, -0.693147182f, -c));      // -c - t ln 2
+    const float p = __builtin_amdgcn_exp2f(t), e = fmaf(p, lost, p), d = 1.0f + e;
+    const float r = __builtin_amdgcn_rcpf(d), s = fmaf(r, fmaf(-d, r, 1.0f), r);
+    rest = e * s;
+    return x < -88.0f ? 0.0f : s;
 }
 
 // e^(-g^2 / 2) to 4 * 2^-24 relative and g^2 2^-29 from the constant, to zero from |g| = 16 on: what the product with log2(e) and (unless SQUARE: g has at most
 // 12 bits, its square is exact) the square lose, up to 1.2 g^2 2^-24 together, goes into the power to first order.  Gradients take it, as logistic_exact (of
-// bfloat16 16384 x 4096: 127 us, with exp_f32 123).
+// bfloat16 16384 x 4096: 122 to 127 us, with exp_f32 121 to 124; 4096 x 1024 13.5 and 13.1).
 template <bool SQUARE> QMM_DEV float exp_half_square(float g)
 {
     const float z = __builtin_amdgcn_fmed3f(g, -16.0f, 16.0f), half = -0.5f * z, s = z * half, t = s * 1.44269504f;

@@ -3,8 +3,8 @@
 // for a token's whole row (g | u), as values for the weight gradient and, quantized with one step size per token (Eq. 1), as the
 // codes of the data gradient's operand.  A row is read once, its 2 F results stay in registers until their largest magnitude is known:
 // the codes are of the binary32 results, not of their bfloat16 roundings.
-// Bound by memory traffic: bfloat16 reads 6 bytes and writes 4 + 2 a pair; 16384 x 4096 (805 MB) 122 us, 6.6 TB/s; GELU's, with more
-// vector work, 125 to 127.
+// Bound by memory traffic: bfloat16 reads 6 bytes and writes 4 + 2 a pair; 16384 x 4096 (805 MB) 120 us, 6.7 TB/s; GELU's, with more
+// vector work, 122 to 127.
 #include "qmm_activation.h"
 #include "qmm_rows.h"
 

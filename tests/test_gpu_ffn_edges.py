@@ -109,8 +109,8 @@ def test_product_keeps_the_stated_accuracy_in_the_tail(kind, m):
 
 
 def test_silu_slope_keeps_its_accuracy():
-    # s (1 + g (1 - s)), in units of 2^-24: s 5 (see test_logistic_keeps_its_accuracy_in_the_tail: power 3, sum, last step), 1 - s as e^-g s 3 + 5 + 1 (for
-    # g < 0 by subtraction: 5 s + 1 / 2, less), the sum's and the product's rounding, 1 for what is of second order
+    # s (1 + g (1 - s)), in units of 2^-24: s 5 (see test_logistic_keeps_its_accuracy_in_the_tail: power 3, sum, last step), 1 - s as e^-g s 3 + 5 + 1,
+    # the sum's and the product's rounding, 1 for what is of second order
     g = torch.cat([torch.linspace(-79.9, 79.9, 20001), torch.linspace(0, 20, 20001), torch.tensor([0.0, -0.0, 1e-30, -1e-30])])
     dg, _ = gated_grad_of(g, torch.ones_like(g), qmm.SILU)
     z = g.double()
