@@ -364,7 +364,8 @@ qmm_status qmm_gemm_gated(const qmm_operand* a, const qmm_operand* b, int64_t ba
  * as values (for the weight gradient, whose operand is quantized along the other axis) and as codes with one step size per row
  * (the data gradient's operand [batch][rows][2 F], per_channel = 1, batch_groups = batch): what qmm_scale and qmm_quantize give for the
  * binary32 results.
- *   dh [..][F], gu [..][2 F]   tensors of one type, batch and rows, contract_axis 1, 2 F up to 2^22.
+ *   dh [..][F], gu [..][2 F]   tensors of one type, batch and rows, contract_axis 1, 2 F up to 2^22 (the K of the data gradient's product, as for
+ *               qmm_gemm).
  *   dgu_out     device, dense [batch][rows][2 F], their type; or NULL.  May be gu's memory where that is dense.
  *   delta_out, codes_out   device; both or neither NULL.  At least one of codes_out and dgu_out.
  * Random bits of stochastic rounding as in qmm_quantize.  Errors as for qmm_rmsnorm_quantize.  Uses no workspace.

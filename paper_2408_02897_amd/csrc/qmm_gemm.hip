@@ -223,7 +223,8 @@ QMM_DEV uint32_t pack_bf16(float a, float b)
 // lines by the 256 x 256 tiles.  (256 workgroups writing nothing but such tiles: 4.6 TB/s; with 64 bytes of a line
 // a wavefront, the layout of the plain product, 2.9, and with 4 or 8 bytes a lane the stores' addresses take longer than all else.)
 // next() is called in front of every unit.  h, gu: token 0 of the block, the wavefront's first column; the block's lane j is token T j.  Streaming stores, as the plain
-// product's of this size (gemm_stream_kernel): kept by the L2 they cost a training step's product 209 us instead of 179.
+// product's of this size (gemm_stream_kernel): kept by the L2 they cost a training step's product 209 us instead of 179
+// (16384 x 4096; measured at that size alone, taken at every one).
 // whole: the block lies inside the matrix and its rows begin on 16-byte boundaries.  Else rows and columns behind the matrix's are left out and the
 // stores are ordinary ones at element boundaries (rows_left, cols_left: from the block's first token and the wavefront's first column on).
 template <bool F8, int NP, int T, int ACT, bool BF, bool GU, typename Value, typename Next>
@@ -2830,7 +2831,8 @@ int plan_splits(int64_t M, int64_t N, int64_t rowbytes, int64_t batch, int fuse)
 // The same for gated products of M tokens: up to 64 of them the workgroups of 16 columns of gated_few_kernel, of which a CU takes two; else 128 x 128
 // tiles (64 columns of both halves), one a CU.  The second kernel takes 3 to 4 us and more where the parts are large, an unsplit product 0.6 us a slab: split
 // from 48 slabs on, or 24 where at most 32 tiles would work (E4M3, unsplit / split: one token 512 x 8192 11.5 / 7.5 us, 1000 x 2000 5.1 / 7.0,
-// 64 tokens 1024 x 8192 25.5 / 16.8; 128 tokens 1024 x 4096 22 / 15.8, 256 x 512 x 8192 37 / 17; 256 x 1024 x 2048 13.0 / 16.3, 128 x 8192 x 4096 22 / 30).
+// 64 tokens 1024 x 8192 25.5 / 16.8; 128 tokens 1024 x 4096 22 / 15.8, 256 x 512 x 8192 37 / 17; 256 x 1024 x 2048 13.0 / 16.3, 128 x 8192 x 4096 22 / 30).  From 33 tiles on nothing
+// is split however long K is, which is too early for very long ones: bfloat16 128 x 4096 x 8192, 64 tiles of 128 slabs, 93 us, the plain product of that size 45.
 // The second kernel's grid has the tokens and matrices for dimensions.
 int plan_gated_splits(int64_t M, int64_t F, int64_t rowbytes, int64_t batch)
 {
@@ -3066,13 +3068,13 @@ qmm_status launch_gated_few(GemmArgs& g, hipStream_t s)
     return run(std::integral_constant<int, 4>{}, W8{});
 }
 
-// Gated products: the tiles of the plain product of the same size, by its rule (launch_fuse).
+// Gated products: the tiles of the plain product of the same size, by its rule (launch_fuse), whose border was measured on plain products.
 template <int KIND, int FA, int FB>
 qmm_status launch_gated(GemmArgs& g, hipStream_t s)
 {
     if (g.N <= kGatedFew) return launch_gated_few<KIND, FA, FB>(g, s);
     // Several whole tiles per CU, 16384 x 4096 x 1024 with (g | u), gemm_kernel / gemm_stream_kernel: E4M3 181 / 165 us, bfloat16 270 / 262.  Not for INT8, whose
-    // epilogue has no registers left beside the stream's (spilled, 190 against 187).
+    // epilogue has no registers left beside the stream's where a lane holds 16 rows of a block, as by the 32 x 32 instructions (spilled, 190 against 187).
     if (g.splits > 1) return launch_tile<KIND, FA, FB, 2, 1, 2, 0, 0, 1>(g, s);
     if constexpr (KIND != KIND_I8) {
         if (use_stream(g, 0)) return launch_stream<KIND, FA, FB, 1>(g, s);
