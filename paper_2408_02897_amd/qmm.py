@@ -600,14 +600,16 @@ def quantize_blocks(x, contract_axis, fmt, block_rows=1, mode=RTNE, seed=0, offs
 
 
 def block_operand(codes, fmt, delta, block_rows=1):
-    """One side of gemm_blocks: uint8 codes [rows, K] or [batch, rows, K] and their step sizes as quantize_blocks gives them."""
+    """One side of gemm_blocks: uint8 codes [rows, K] or [batch, rows, K] and their step sizes as quantize_blocks gives them: [batch, blocks of 128 along K, rows of
+    blocks], without its first axis for one matrix, or those values in a row.  (In another order, such as [rows, blocks], as many values are another matrix's.)"""
     if codes.dtype != torch.uint8 or codes.dim() not in (2, 3) or not codes.is_contiguous():
         raise ValueError("codes are a contiguous uint8 tensor [rows, K] or [batch, rows, K]")
     if block_rows not in (1, BLOCK):
         raise ValueError("block_rows is 1 or 128")
     batch, rows, k = codes.shape if codes.dim() == 3 else (1, *codes.shape)
     need = _block_scales(batch, rows, k, block_rows)
-    if delta.dtype != torch.float32 or not delta.is_contiguous() or delta.numel() != need[0] * need[1] * need[2] or delta.device != codes.device:
+    shapes = (need, (need[0] * need[1] * need[2],), *([need[1:]] if batch == 1 else []))
+    if delta.dtype != torch.float32 or not delta.is_contiguous() or tuple(delta.shape) not in shapes or delta.device != codes.device:
         raise ValueError(f"step sizes {tuple(delta.shape)} of {delta.dtype}, not {need} of float32 side by side on the codes' device")
     op = BlockOperand(codes.data_ptr(), fmt, block_rows, delta.data_ptr())
     op._keep = (codes, delta)

@@ -175,3 +175,16 @@ def test_binding_refuses():
                 lambda: qmm.layernorm_quantize(x, None, None), lambda: qmm.layernorm_backward(x, x, torch.zeros(4), torch.ones(4), None)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_step_sizes_in_another_order_are_refused():
+    """As many step sizes as the operand has, laid out [rows, blocks] or for other matrices: another matrix's, by the product's rule."""
+    for codes, per, good, bad in ((torch.zeros((256, 256), dtype=torch.uint8), 1, ((512,), (2, 256), (1, 2, 256)), ((256, 2), (1, 256, 2), (2, 256, 1), (2, 1, 256), (1, 1, 2, 256))),
+                                  (torch.zeros((300, 1024), dtype=torch.uint8), 128, ((24,), (8, 3), (1, 8, 3)), ((3, 8), (1, 3, 8), (8, 3, 1))),
+                                  (torch.zeros((2, 40, 272), dtype=torch.uint8), 1, ((240,), (2, 3, 40)), ((2, 40, 3), (3, 80), (6, 40), (3, 2, 40), (3, 40, 2))),
+                                  (torch.zeros((1, 40, 272), dtype=torch.uint8), 1, ((120,), (3, 40), (1, 3, 40)), ((40, 3), (1, 40, 3)))):
+        for shape in good:
+            qmm.block_operand(codes, qmm.E4M3, torch.ones(shape), block_rows=per)
+        for shape in bad:
+            with pytest.raises(ValueError, match="step sizes"):
+                qmm.block_operand(codes, qmm.E4M3, torch.ones(shape), block_rows=per)
