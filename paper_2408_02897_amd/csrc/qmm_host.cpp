@@ -472,7 +472,7 @@ PyObject* quantize_blocks(PyObject*, PyObject* const* args, Py_ssize_t n)
 
 PyTypeObject* block_type = nullptr;            // qmm.BlockOperand, the ctypes structure of a qmm_block_operand
 
-// The operand of a pair (codes, BlockOperand), if it was made for this tensor (_check_block_operand of qmm.py).
+// The operand of a pair (codes, BlockOperand), if it was made for this tensor and has a step size for every block (_check_block_operand of qmm.py).
 bool block_of(PyObject* pair, const at::Tensor** data, qmm_block_operand* op)
 {
     if (!block_type || !PyTuple_CheckExact(pair) || PyTuple_GET_SIZE(pair) != 2 || !plain(PyTuple_GET_ITEM(pair, 0)) || Py_TYPE(PyTuple_GET_ITEM(pair, 1)) != block_type)
@@ -491,7 +491,9 @@ bool block_of(PyObject* pair, const at::Tensor** data, qmm_block_operand* op)
     bool good = PyTuple_CheckExact(keep) && PyTuple_GET_SIZE(keep) == 2 && plain(PyTuple_GET_ITEM(keep, 0)) && plain(PyTuple_GET_ITEM(keep, 1));
     if (good) {
         const at::Tensor &own = THPVariable_Unpack(PyTuple_GET_ITEM(keep, 0)), &delta = THPVariable_Unpack(PyTuple_GET_ITEM(keep, 1));
-        good = own.data_ptr() == t.data_ptr() && own.sizes() == t.sizes() && op->data == t.data_ptr() && op->delta == delta.data_ptr() && here(delta);
+        const int64_t d = t.dim();
+        good = (d == 2 || d == 3) && own.data_ptr() == t.data_ptr() && own.sizes() == t.sizes() && op->data == t.data_ptr() && op->delta == delta.data_ptr() && here(delta) &&
+               qmm_num_block_scales(d == 3 ? t.size(0) : 1, t.size(d - 2), t.size(d - 1), op->block_rows) == delta.numel();
     }
     Py_DECREF(keep);
     return good;

@@ -617,7 +617,14 @@ def block_operand(codes, fmt, delta, block_rows=1):
 
 
 def _check_block_operand(t, op):
-    if op._keep[0].data_ptr() != t.data_ptr() or op._keep[0].shape != t.shape or op.data != op._keep[0].data_ptr() or op.delta != op._keep[1].data_ptr():
+    """An operand reads what its tensors hold: the codes it was made for, and a step size for every block (block_rows may have been set since)."""
+    codes, delta = getattr(op, "_keep", (None, None))
+    if codes is None:
+        raise ValueError("not an operand that block_operand made")
+    need = _block_scales(*(codes.shape if codes.dim() == 3 else (1, *codes.shape)), op.block_rows)
+    if op.block_rows in (1, BLOCK) and delta.numel() != need[0] * need[1] * need[2]:
+        raise ValueError(f"{delta.numel()} step sizes, not {need}")
+    if codes.data_ptr() != t.data_ptr() or codes.shape != t.shape or op.data != codes.data_ptr() or op.delta != delta.data_ptr():
         if t.numel():
             raise ValueError("an operand of another tensor")
 

@@ -188,3 +188,19 @@ def test_step_sizes_in_another_order_are_refused():
         for shape in bad:
             with pytest.raises(ValueError, match="step sizes"):
                 qmm.block_operand(codes, qmm.E4M3, torch.ones(shape), block_rows=per)
+
+
+def test_operands_changed_since_they_were_made_are_refused():
+    """With block_rows set to 1 where there are step sizes per 128 rows the product would read past them."""
+    codes, other = torch.zeros((300, 256), dtype=torch.uint8), torch.zeros((300, 256), dtype=torch.uint8)
+    make = lambda per: qmm.block_operand(codes, qmm.E4M3, torch.ones((2, -(-300 // per))), block_rows=per)
+    for per in (1, 128):
+        qmm._check_block_operand(codes, make(per))
+        op = make(per)
+        op.block_rows = 129 - per
+        with pytest.raises(ValueError, match="step sizes"):
+            qmm._check_block_operand(codes, op)
+        with pytest.raises(ValueError, match="another tensor"):
+            qmm._check_block_operand(other, make(per))
+    with pytest.raises(ValueError, match="block_operand"):
+        qmm._check_block_operand(codes, qmm.BlockOperand(codes.data_ptr(), qmm.E4M3, 1, 0))

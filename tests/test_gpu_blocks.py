@@ -279,6 +279,18 @@ def test_operands_of_other_tensors():
             qmm.gemm_blocks(*bad)
 
 
+@pytest.mark.parametrize("short", [None, qmm._NoShortPath])
+def test_operands_changed_since_they_were_made(short, monkeypatch):
+    monkeypatch.setattr(qmm, "_short", short)
+    for per_a, per_b in ((1, 128), (128, 1)):
+        for which in range(2):
+            pairs = operands(3, 1, 200, 300, 256, qmm.E4M3, qmm.E4M3, per_a, per_b)[:2]
+            qmm.gemm_blocks(*pairs)
+            pairs[which][1].block_rows = 129 - pairs[which][1].block_rows
+            with pytest.raises(ValueError, match="step sizes"):
+                qmm.gemm_blocks(*pairs)
+
+
 @pytest.mark.parametrize("m,n,k", [(300, 1000, 8192), (100, 512, 4096), (4096, 3328, 256)])
 def test_products_recorded_and_at_once(m, n, k):
     """Two graphs of the same product (parts of a contraction in a workspace of each one's own; workgroups that stay) replayed in turn and side by side, codes
