@@ -455,7 +455,7 @@ qmm_status qmm_dropout(const qmm_tensor* x, float p, uint64_t seed, uint64_t off
  *   delta_out, codes_out  device, both NULL: no quantization (fmt, block, mode are then not looked at).
  * Random bits of stochastic rounding as in qmm_quantize.  The mean is subtracted before the squares are summed, and what its rounding left is taken out
  * again: a row's offset does not cost its variance's accuracy.  A row whose squares overflow binary32 has rstd 0 and y = bias; a row with an inf or
- * NaN, or whose sum overflows, has y NaN, delta NaN and codes 0x7F (INT8 0).  Where all of a row's differences are zero (and eps = 0) y = bias.  cols = 0: delta 1
+ * NaN, or whose sum overflows, has y NaN, delta NaN and codes 0x7F (INT8 0).  Where all of a row's differences are zero and eps = 0, its rstd is infinite and y = bias.  cols = 0: delta 1
  * (block = 0), mean 0, rstd 1 / sqrt(eps).  Uses no workspace.  Errors as for qmm_rmsnorm_quantize; dropout outside 0 to 1: QMM_ERR_SHAPE; block: QMM_ERR_ENUM.
  */
 qmm_status qmm_layernorm_quantize(const qmm_tensor* x, const qmm_tensor* residual, const void* weight, const void* bias, qmm_dtype weight_dtype,
@@ -468,6 +468,7 @@ qmm_status qmm_layernorm_quantize(const qmm_tensor* x, const qmm_tensor* residua
  *     a = weight * dy,  n = (h - mean) * rstd,  dh = rstd * (a - mean_j(a) - n * mean_j(a n)) + dresidual
  *     dx = dh's dropout (that of the forward pass: same dropout, seed and offset),  dw = sum over all rows of dy n,  db = sum over all rows of dy
  * dh is the gradient of the residual, dx that of x (dropout = 0: dh is both, and dx_out is not written).
+ * A row whose rstd is infinite (no spread, eps = 0) has n = 0 as in the forward pass: its dh is dresidual, or 0, it adds nothing to dw and dy to db.
  *   dy, h, dresidual   tensors of one extent and type, contract_axis 1; dresidual (the gradient that reaches h past the norm) or NULL.
  *   mean, rstd         device, batch * rows floats, as qmm_layernorm_quantize wrote them.
  *   dh_out, dx_out     device, dense, their type; each may be the memory of one of the inputs where that is dense.

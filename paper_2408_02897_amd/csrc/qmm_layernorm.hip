@@ -67,8 +67,10 @@ template <int PER> QMM_DEV int64_t unit_of(int64_t blk, int64_t units)
     return blk - r + (r % 8) * RUN + r / 8;
 }
 
+// 1 / root as what multiplies the differences: of a row without a spread (variance 0 and eps 0, infinite) they count as zero in both passes, not as zero times infinity.
+QMM_DEV float slope_of(float rstd) { return rstd == __uint_as_float(0x7F800000u) ? 0.0f : rstd; }
 struct Stats { float mean, rest, rstd, factor; };
-// From the sums of d and d^2.  A row without a spread (variance 0 and eps 0) has v 0, not zero times infinity.
+// From the sums of d and d^2.
 QMM_DEV Stats stats_of(float mean, float sum_d, float sum_d2, int64_t cols, float eps)
 {
     const float n = cols > 0 ? (float)cols : 1.0f, off = sum_d / n, var = fmaf(-off, off, sum_d2 / n);
@@ -78,7 +80,7 @@ QMM_DEV Stats stats_of(float mean, float sum_d, float sum_d2, int64_t cols, floa
     Stats s;
     s.mean = mean + rest; s.rest = rest;
     s.rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);                  // (NaN stays)
-    s.factor = s.rstd == __uint_as_float(0x7F800000u) ? 0.0f : s.rstd;
+    s.factor = slope_of(s.rstd);
     return s;
 }
 
@@ -408,6 +410,7 @@ layernorm_grad_rows(LayerGradArgs a)
         Row next;
         if constexpr (AHEAD) { if ((blk + gridDim.x) * RPB < total) fetch(blk + gridDim.x, next); }
         else { fetch(blk, row); load_weights(); }
+        const float rstd = slope_of(row.rstd);
         float sum_a = 0.0f, sum_an = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -418,7 +421,7 @@ layernorm_grad_rows(LayerGradArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 // (behind the row's end dy is zero; n may be anything finite or not, so it is left out there)
-                const float d = Vec<T>::at(row.g[k], e), n = c + e < cols ? (Vec<T>::at(row.w[k], e) - row.mean) * row.rstd : 0.0f, g = d * weight[k][e];
+                const float d = Vec<T>::at(row.g[k], e), n = c + e < cols ? (Vec<T>::at(row.w[k], e) - row.mean) * rstd : 0.0f, g = d * weight[k][e];
                 sum_a += g;
                 sum_an = fmaf(g, n, sum_an);
                 dw[k][e] = fmaf(d, n, dw[k][e]);
@@ -434,8 +437,8 @@ layernorm_grad_rows(LayerGradArgs a)
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float n = (Vec<T>::at(row.w[k], e) - row.mean) * row.rstd;
-                v[e] = fmaf(row.rstd, fmaf(-n, mean_an, Vec<T>::at(row.g[k], e) * weight[k][e] - mean_a), Vec<T>::at(row.q[k], e));
+                const float n = (Vec<T>::at(row.w[k], e) - row.mean) * rstd;
+                v[e] = fmaf(rstd, fmaf(-n, mean_an, Vec<T>::at(row.g[k], e) * weight[k][e] - mean_a), Vec<T>::at(row.q[k], e));
             }
             store_gradients<T, false>(a, id * a.cols + c, v, left);
         }
@@ -487,7 +490,7 @@ layernorm_grad_long(LayerGradArgs a)
         const T* dy = static_cast<const T*>(a.dy) + b * a.dy_batch + i * a.dy_row;
         const T* h = static_cast<const T*>(a.h) + b * a.h_batch + i * a.h_row;
         const T* r = a.r ? static_cast<const T*>(a.r) + b * a.r_batch + i * a.r_row : nullptr;
-        const float mean = a.mean[id], rstd = a.rstd[id];
+        const float mean = a.mean[id], rstd = slope_of(a.rstd[id]);
         float sum_a = 0.0f, sum_an = 0.0f;
         for (int c = (int)threadIdx.x * V; c < cols; c += kRowLanes * V) {
             const u32x4 g = load_row<T>(dy, c, cols), w = load_row<T>(h, c, cols);
@@ -529,7 +532,7 @@ layernorm_grad_columns(LayerGradArgs a)                // grid (columns, shares)
         const int64_t b = a.batch > 1 ? id / a.rows : 0, i = id - b * a.rows;
         const u32x4 g = load_row<T>(static_cast<const T*>(a.dy) + b * a.dy_batch + i * a.dy_row, (int)c, (int)a.cols);
         const u32x4 w = load_row<T>(static_cast<const T*>(a.h) + b * a.h_batch + i * a.h_row, (int)c, (int)a.cols);
-        const float mean = a.mean[id], rstd = a.rstd[id];
+        const float mean = a.mean[id], rstd = slope_of(a.rstd[id]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float d = Vec<T>::at(g, e);
