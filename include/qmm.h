@@ -429,7 +429,7 @@ qmm_status qmm_gemm_blocks(const qmm_block_operand* a, const qmm_block_operand* 
 /*
  * qmm_dropout -- out = x * 1 / (1 - p) where an element is kept, 0 (whatever x is there) where it is dropped.  The decisions are functions of (seed,
  * offset + the element's linear index in out) and are not stored: the gradient is the same call on the upstream gradient.
- *   Element number n = index + offset has 16 random bits u: half n % 2 (0: the low one) of word (n % 8) / 2 of Philox4x32-10 with counter (n / 8 as two
+ *   Element number n = index + offset (modulo 2^64) has 16 random bits u: half n % 2 (0: the low one) of word (n % 8) / 2 of Philox4x32-10 with counter (n / 8 as two
  *   32-bit halves, 1, 0) and key = seed as two halves (the 1 keeps these bits apart from those of stochastic rounding).  It is dropped iff u < T,
  *   T = p * 65536 rounded to nearest; what is kept is multiplied by 65536 / (65536 - T) in binary32, the reciprocal of the probability that is used
  *   (p to within 2^-17), and rounded once to x's type.

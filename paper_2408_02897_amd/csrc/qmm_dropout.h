@@ -37,7 +37,7 @@ template <int V> QMM_DEV Kept kept(const Drop& d, uint64_t n)
         uint64_t q2 = 0, q3 = 0;
         if (__any(j + V > 8u)) {
             asm volatile("; parts of blocks");           // (keeps the compiler from computing this for every call and selecting)
-            words(c + 1, q2, q3);
+            words((n + 8) >> 3, q2, q3);         // (behind the last number comes number 0: element counts are modulo 2^64)
         }
         if (j & 4u) { q0 = q1; q1 = q2; q2 = q3; }
         const uint32_t away = (j & 3u) * 16u;

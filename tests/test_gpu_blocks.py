@@ -346,3 +346,16 @@ def test_dropout_of_a_whole_and_its_parts():
     got = qmm.dropout(special, 0.5, 9).cpu()
     assert torch.all(got[~keep] == 0) and torch.isnan(got[keep][0::1][torch.isnan(special.cpu()[keep])]).all()
     assert qmm.dropout(torch.empty((0, 5), device=DEV), 0.1, 0).shape == (0, 5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_dropout_numbers_start_again_behind_the_last(dtype):
+    """Element numbers are modulo 2^64: within a vector that holds the last and the first of them too, for offsets given as negative numbers as well."""
+    x = torch.ones((2, 40), dtype=dtype)
+    for back in range(1, 18):
+        for seed in range(4):
+            want = B.dropped(x, 0.5, seed, 2 ** 64 - back)
+            for offset in (2 ** 64 - back, -back):
+                assert R.same_bits(qmm.dropout(x.to(DEV), 0.5, seed, offset), want)
+            whole = qmm.dropout(torch.ones((1, 40 + back), dtype=dtype, device=DEV), 0.5, seed, -back)
+            assert R.same_bits(whole[:, back:], qmm.dropout(torch.ones((1, 40), dtype=dtype, device=DEV), 0.5, seed, 0))
