@@ -687,6 +687,7 @@ def layernorm_quantize(x, weight, bias, fmt=None, block=False, residual=None, ep
     w_ptr, w_type = _weight_args(weight, t.cols)
     b_ptr, b_type = _weight_args(bias, t.cols)
     assert weight is None or bias is None or w_type == b_type, "weight and bias of one type"
+    dropout = ctypes.c_float(dropout).value                    # as the library gets it: what is 0 there makes no h
     new_h = residual is not None or dropout > 0
     h = x
     if new_h:
@@ -722,6 +723,7 @@ def layernorm_backward(dy, h, mean, rstd, weight, dresidual=None, dropout=0.0, d
     for s in (mean, rstd):
         assert s.dtype == torch.float32 and s.is_contiguous() and s.numel() == t.batch * t.rows, "one mean and rstd per row"
     dh = torch.empty(dy.shape, dtype=dy.dtype, device=dev) if dh_out is None else _dense_out(dh_out, dy.shape, dy.dtype)
+    dropout = ctypes.c_float(dropout).value                    # as the library gets it: with 0 there is no dx
     if dropout > 0:
         dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev) if dx_out is None else _dense_out(dx_out, dy.shape, dy.dtype)
     else:
