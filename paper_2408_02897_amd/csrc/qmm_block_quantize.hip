@@ -228,7 +228,7 @@ block_tiles(BlockArgs a, uint32_t tiles_c, uint32_t tiles_r, int64_t tiles)
 template <typename T, int FMT, int MODE> qmm_status launch_blocks(const BlockArgs& a, bool square, hipStream_t s)
 {
     const int64_t tiles_c = (a.cols + kBlock - 1) / kBlock, tiles_r = (a.rows + kBlock - 1) / kBlock, tiles = tiles_c * tiles_r * a.batch;
-    const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 22);
+    const unsigned grid = (unsigned)std::min<int64_t>(tiles, ((int64_t)1 << 31) / kTileThreads<T>);       // (a launch takes less than 2^32 threads; the others follow in turn)
 #define QMM_TILES(SQ, R, C) block_tiles<T, FMT, MODE, SQ, R, C><<<grid, kTileThreads<T>, 0, s>>>(a, (uint32_t)tiles_c, (uint32_t)tiles_r, tiles)
     if (square) {
         if (a.codes && a.codes_t) QMM_TILES(true, true, true);

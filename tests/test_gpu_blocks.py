@@ -189,6 +189,18 @@ def test_elements_past_32_bits():
     assert R.same_bits(g.dh.reshape(-1, cols)[before:], q.dh.reshape(-1, cols)) and R.same_bits(g.dx.reshape(-1, cols)[before:], q.dx.reshape(-1, cols))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_codes_of_more_tiles_than_a_launch_takes(dtype):
+    """65535 matrices of one row: 65 tiles each, in all more than 2^32 threads' worth in binary32.  Row by row they are those of one matrix with as many rows."""
+    x = torch.randn((65535, 1, 8320), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV, dtype=dtype)
+    want, step = qmm.quantize_blocks(x[:, 0], 1, qmm.E4M3)
+    (c, d), (ct, dt) = qmm.quantize_blocks(x, 1, qmm.E4M3, both=True)
+    assert torch.equal(c[:, 0], want[0]) and torch.equal(d[:, :, 0], step[0].t())
+    for first, last in ((0, 3), (32767, 32771), (65532, 65535)):
+        pt, pdt = qmm.quantize_blocks(x[first:last], 0, qmm.E4M3)
+        assert torch.equal(ct[first:last], pt) and torch.equal(dt[first:last], pdt)
+
+
 # ------------------------------------------------------------------------------------------------ product
 def operands(seed, batch, m, n, k, fa, fb, per_a, per_b):
     x, w = normal(seed, batch, m, k, scale=2.0).to(DEV), normal(seed + 1, batch, n, k, scale=0.05).to(DEV)
