@@ -3,6 +3,7 @@
 import pytest
 import torch
 
+import block_forms as F
 import block_reference as B
 import ffn_reference as R
 from paper_2408_02897_amd import qmm
@@ -243,6 +244,36 @@ def test_product_of_many_tiles(m, n, k):
         check_product(*operands(k, 1, m, n, k, qmm.E5M2, qmm.E4M3, per_a, per_b))
 
 
+@pytest.mark.parametrize("batch,m,n,k,tile,splits,groups", F.FORMS)
+def test_product_by_every_form(batch, m, n, k, tile, splits, groups):
+    """Step sizes per row and per 128 rows of either operand, both output types; what lies around the output stays as it was."""
+    for fa, fb, per_a, per_b in ((qmm.E4M3, qmm.E4M3, 1, 128), (qmm.E5M2, qmm.E4M3, 1, 1), (qmm.E4M3, qmm.E5M2, 128, 128)):
+        a, b, what = operands(m + n + k, batch, m, n, k, fa, fb, per_a, per_b)
+        check_product(a, b, what)
+        for dtype in (F32, BF):
+            room = torch.full((batch * m * n + 4096,), 7.0, dtype=dtype, device=DEV)
+            out = room[2048:-2048].view(batch, m, n)
+            qmm.gemm_blocks(a, b, out=out)
+            assert torch.all(room[:2048] == 7) and torch.all(room[-2048:] == 7) and torch.equal(out, qmm.gemm_blocks(a, b, dtype))
+
+
+@pytest.mark.parametrize("batch,m,n,k,tile,splits,groups", F.LARGE[:3] + F.LARGE_SPLIT[1:4] + F.MIDDLE[:2] + F.MIDDLE_SPLIT[3:5] + F.SMALL[1:2] + F.FEW[1:3])
+def test_not_a_number_in_one_row(batch, m, n, k, tile, splits, groups):
+    """Codes and step sizes that are not finite reach their rows' and columns' outputs and no others, those of a workgroup's next tile among them."""
+    for per_b in (1, 128):
+        a, b, what = operands(5, batch, m, n, k, qmm.E4M3, qmm.E4M3, 1, per_b)
+        want = qmm.gemm_blocks(a, b, F32)
+        ca, cb, da, db = (t.clone() for t in what[:4])
+        i, j, z = m // 2, n - 1, batch - 1
+        ca[z, i, k - 1] = 0x7F
+        cb[z, j, 0] = 0x7F
+        da[z, -1, 0] = float("nan")
+        got = qmm.gemm_blocks((ca, qmm.block_operand(ca, qmm.E4M3, da)), (cb, qmm.block_operand(cb, qmm.E4M3, db, block_rows=per_b)), F32)
+        hit = torch.zeros((batch, m, n), dtype=torch.bool, device=DEV)
+        hit[z, i], hit[z, :, j], hit[z, 0] = True, True, True
+        assert torch.equal(torch.isnan(got), hit) and torch.equal(got[~hit], want[~hit])
+
+
 @pytest.mark.parametrize("m,n", [(1, 64), (40, 70), (100, 200), (300, 130), (4096, 3200)])
 def test_a_block_is_the_plain_products_sum(m, n):
     """One block and step sizes of one: the accumulators of qmm_gemm, bit for bit."""
@@ -332,6 +363,13 @@ def test_products_recorded_and_at_once(m, n, k):
         torch.cuda.synchronize()
         for i, (g, y, parts) in enumerate(runs):
             assert R.same_bits(y, want[(turn + i) % 3])
+
+
+@pytest.mark.parametrize("batch,m,n,k,tile,splits,groups", [F.LARGE[0], F.LARGE_SPLIT[0], F.LARGE_SPLIT[2], F.MIDDLE_SPLIT[0], F.MIDDLE_SPLIT[1]])
+def test_products_of_large_forms_recorded_and_at_once(batch, m, n, k, tile, splits, groups):
+    """Workgroups that go from tile to tile, and parts of a contraction in 256 x 256 and 128 x 128, in two graphs side by side."""
+    assert batch == 1
+    test_products_recorded_and_at_once(m, n, k)
 
 
 # ------------------------------------------------------------------------------------------------ dropout
