@@ -767,27 +767,27 @@ qmm_status launch_reduce(const BlockGemmArgs& g, hipStream_t s)
 template <int FA, int FB, int WN, int WM, int TN, int TM, int SLOTS, bool PER_ROW> qmm_status launch_tiles(BlockGemmArgs& g, hipStream_t s)
 {
     constexpr int BN = 16 * WN * TN, BM = 16 * WM * TM, LDS_BYTES = SLOTS * (BN + BM) * (kBlock + 4);
-    static_assert(LDS_BYTES <= 160 * 1024, "LDS of a CU");
-    const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN, total = tm * tn * g.batch * g.splits;
-    if (total > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;
+    static_assert(LDS_BYTES <= 160 * 1024 && 64 * WN * WM == kTileThreads, "LDS of a CU, threads of a workgroup");
+    const int64_t tm = (g.M + BM - 1) / BM, tn = (g.N + BN - 1) / BN;
+    if (!launches((double)tm * tn * g.batch * g.splits, kTileThreads)) return QMM_ERR_UNSUPPORTED;      // (no contraction: every other plan fits)
     g.tiles_m = (int)tm; g.tiles_n = (int)tn;
     auto kern = block_gemm<FA, FB, WN, WM, TN, TM, SLOTS, PER_ROW>;
     static std::atomic<uint64_t> done{0};
     if (!ensure_lds(done, reinterpret_cast<const void*>(kern), LDS_BYTES)) return QMM_ERR_LAUNCH;
-    kern<<<(unsigned)total, 64 * WN * WM, LDS_BYTES, s>>>(g);
+    kern<<<(unsigned)(tm * tn * g.batch * g.splits), 64 * WN * WM, LDS_BYTES, s>>>(g);
     return g.splits > 1 ? launch_reduce(g, s) : launch_status();
 }
 constexpr int kLargeGrid = 256;                // one workgroup of the large tile a CU
 template <int FA, int FB, bool PER_ROW> qmm_status launch_large(BlockGemmArgs& g, hipStream_t s)
 {
     constexpr int LDS_BYTES = 2 * 512 * (kBlock + 4);
-    const int64_t tm = (g.M + 255) / 256, tn = (g.N + 255) / 256, total = tm * tn * g.batch * g.splits;
-    if (total > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;
+    const int64_t tm = (g.M + 255) / 256, tn = (g.N + 255) / 256;
+    if ((double)tm * tn * g.batch * g.splits > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;      // (in binary64: the product may pass 64 bits)
     g.tiles_m = (int)tm; g.tiles_n = (int)tn;
     auto kern = block_gemm_large<FA, FB, PER_ROW>;
     static std::atomic<uint64_t> done{0};
     if (!ensure_lds(done, reinterpret_cast<const void*>(kern), LDS_BYTES)) return QMM_ERR_LAUNCH;
-    kern<<<(unsigned)std::min<int64_t>(total, kLargeGrid), 512, LDS_BYTES, s>>>(g);
+    kern<<<(unsigned)std::min<int64_t>(tm * tn * g.batch * g.splits, kLargeGrid), 512, LDS_BYTES, s>>>(g);
     return g.splits > 1 ? launch_reduce(g, s) : launch_status();
 }
 template <int FA, int FB, bool PER_ROW> qmm_status launch_form(BlockGemmArgs& g, int tile, hipStream_t s)
@@ -796,12 +796,12 @@ template <int FA, int FB, bool PER_ROW> qmm_status launch_form(BlockGemmArgs& g,
     if (tile == 128) return launch_tiles<FA, FB, 2, 2, 4, 4, 2, PER_ROW>(g, s);
     if (tile == 64) return launch_tiles<FA, FB, 2, 2, 2, 2, 4, PER_ROW>(g, s);
     const int64_t tn = (g.N + 15) / 16;
-    if (tn * g.batch > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;
+    if (!launches((double)tn * g.batch, kFewThreads)) return QMM_ERR_UNSUPPORTED;
     g.tiles_n = (int)tn;
     const unsigned grid = (unsigned)(tn * g.batch);
-    if (g.M <= 16) block_few<FA, FB, 1, 8, PER_ROW><<<grid, 512, 0, s>>>(g);
-    else if (g.M <= 32) block_few<FA, FB, 2, 8, PER_ROW><<<grid, 512, 0, s>>>(g);
-    else block_few<FA, FB, 4, 8, PER_ROW><<<grid, 512, 0, s>>>(g);
+    if (g.M <= 16) block_few<FA, FB, 1, kFewThreads / 64, PER_ROW><<<grid, kFewThreads, 0, s>>>(g);
+    else if (g.M <= 32) block_few<FA, FB, 2, kFewThreads / 64, PER_ROW><<<grid, kFewThreads, 0, s>>>(g);
+    else block_few<FA, FB, 4, kFewThreads / 64, PER_ROW><<<grid, kFewThreads, 0, s>>>(g);
     return launch_status();
 }
 template <int FA, int FB> qmm_status launch_formats(BlockGemmArgs& g, bool per_row, int tile, hipStream_t s)
@@ -809,6 +809,8 @@ template <int FA, int FB> qmm_status launch_formats(BlockGemmArgs& g, bool per_r
     return per_row ? launch_form<FA, FB, true>(g, tile, s) : launch_form<FA, FB, false>(g, tile, s);
 }
 
+// (the kernels keep 32-bit byte offsets within a tile's rows)
+bool beyond(int64_t M, int64_t N, int64_t K) { return K > (int64_t(1) << 22) || M > 0x7FFFFFFF || N > 0x7FFFFFFF; }
 qmm_status check_block_operand(const qmm_block_operand* o)
 {
     if (!o) return QMM_ERR_NULL;
@@ -825,7 +827,7 @@ using namespace qmm;
 
 extern "C" size_t qmm_gemm_blocks_workspace_size(int64_t batch, int64_t M, int64_t N, int64_t K)
 {
-    if (batch <= 0 || M <= 0 || N <= 0 || K <= 0) return 0;
+    if (batch <= 0 || M <= 0 || N <= 0 || K <= 0 || beyond(M, N, K)) return 0;
     const int splits = plan_of(M, N, K, batch).splits;
     return splits > 1 ? (size_t)splits * (size_t)batch * (size_t)M * (size_t)N * 4u : 0;
 }
@@ -840,7 +842,7 @@ extern "C" qmm_status qmm_gemm_blocks(const qmm_block_operand* a, const qmm_bloc
     if (y_dtype != QMM_DT_BF16 && y_dtype != QMM_DT_F32) return QMM_ERR_ENUM;
     if (batch < 0 || M < 0 || N < 0 || K < 0) return QMM_ERR_SHAPE;
     if (K % 16 != 0) return QMM_ERR_ALIGN;
-    if (K > (int64_t(1) << 22) || M > 0x7FFFFFFF || N > 0x7FFFFFFF) return QMM_ERR_UNSUPPORTED;      // the kernels keep 32-bit byte offsets within a tile's rows
+    if (beyond(M, N, K)) return QMM_ERR_UNSUPPORTED;
     if (batch == 0 || M == 0 || N == 0) return QMM_OK;
     if (!y || (K > 0 && (!a->data || !b->data || !a->delta || !b->delta))) return QMM_ERR_NULL;
     if (!aligned16(a->data) || !aligned16(b->data) || !aligned16(y)) return QMM_ERR_ALIGN;

@@ -54,3 +54,12 @@ def test_the_workspace_is_the_parts(plans):
     from paper_2408_02897_amd import qmm
     for (b, m, n, k), (tile, splits) in zip((f[:4] for f in F.FORMS), plans([f[:4] for f in F.FORMS])):
         assert qmm.lib().qmm_gemm_blocks_workspace_size(b, m, n, k) == (4 * splits * b * m * n if splits > 1 else 0)
+
+
+def test_no_form_asks_for_more_than_a_launch_takes(plans):
+    """Less than 2^32 threads: 512 a workgroup with few tokens, 256 in tiles of 128 and 64; workgroups of 256 x 256 go round."""
+    sizes = [(b, m, n, k) for b in (1, 3, 2 ** 16, 2 ** 23 - 1, 2 ** 23, 2 ** 24 + 1, 2 ** 28) for m in (1, 16, 17, 40, 64, 65, 129, 5000) for n in (1, 16, 17, 4000, 2 ** 28, 2 ** 31 - 1)
+             for k in (16, 128, 4096, 2 ** 22)]
+    for s, (tile, splits) in zip(sizes, plans(sizes)):
+        assert tile == 256 or workgroups(*s[:3], tile, splits) * (512 if tile == 0 else 256) < 2 ** 32, (s, tile, splits)
+    assert plans([(2 ** 24 - 1, 1, 1, 16), (2 ** 24, 1, 1, 16)]) == [(64, 1), (256, 1)]

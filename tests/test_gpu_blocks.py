@@ -372,6 +372,21 @@ def test_products_of_large_forms_recorded_and_at_once(batch, m, n, k, tile, spli
     test_products_recorded_and_at_once(m, n, k)
 
 
+@pytest.mark.parametrize("batch,m", [(2 ** 24 - 1, 1), (2 ** 24 + 5, 2)])
+def test_product_of_more_matrices_than_a_launch_takes(batch, m):
+    """A workgroup a matrix, up to 2^32 threads and beyond."""
+    g = torch.Generator(device=DEV).manual_seed(batch)
+    code = lambda r: torch.randint(0, 0x78, (batch, r, 16), generator=g, device=DEV, dtype=torch.uint8)        # (finite and positive)
+    ca, cb = code(m), code(1)
+    da, db = (torch.rand((batch, 1, r), generator=g, device=DEV) + 0.5 for r in (m, 1))
+    got = qmm.gemm_blocks((ca, qmm.block_operand(ca, qmm.E4M3, da)), (cb, qmm.block_operand(cb, qmm.E4M3, db)), F32)
+    for i in range(m):
+        va, vb = B.decode(ca[:, i], qmm.E4M3), B.decode(cb[:, 0], qmm.E4M3)
+        step = da[:, 0, i].double() * db[:, 0, 0].double()
+        y, cut = (va * vb).sum(1) * step, (B.power(va, qmm.E4M3) * B.power(vb, qmm.E4M3)).sum(1) * step
+        assert torch.all((got[:, i, 0].double() - y).abs() <= 7.0 * 2.0 ** -13 * cut + 32 * R.EPS32 * y + 2.0 ** -120)      # (as in block_reference.product)
+
+
 # ------------------------------------------------------------------------------------------------ dropout
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("shape", [(1, 1), (1, 4096), (3, 7), (67, 100), (2, 9, 129), (3, 50, 8)])
