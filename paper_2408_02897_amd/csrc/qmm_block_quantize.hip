@@ -277,7 +277,7 @@ extern "C" qmm_status qmm_quantize_blocks(const qmm_tensor* x, qmm_format fmt, i
     if (block_rows != 1 && block_rows != kBlock) return QMM_ERR_ENUM;
     if (mode != QMM_ROUND_RTNE && mode != QMM_ROUND_STOCHASTIC) return QMM_ERR_ENUM;
     if (!delta_t_out != !codes_t_out) return QMM_ERR_NULL;
-    if (x->batch > 65535 || x->rows > 0x7FFFFFFF || x->cols > 0x7FFFFFFF - kBlock) return QMM_ERR_UNSUPPORTED;
+    if (x->batch > 65535 || x->rows > 0x7FFFFFFF - kBlock || x->cols > 0x7FFFFFFF - kBlock) return QMM_ERR_UNSUPPORTED;
     if (x->batch == 0 || x->rows == 0 || x->cols == 0) return QMM_OK;
     if (!x->data || !delta_out || !codes_out) return QMM_ERR_NULL;
     if (!element_aligned(x->data, x->dtype) || !element_aligned(delta_out, QMM_DT_F32) || !element_aligned(delta_t_out, QMM_DT_F32)) return QMM_ERR_ALIGN;

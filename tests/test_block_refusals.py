@@ -204,3 +204,12 @@ def test_operands_changed_since_they_were_made_are_refused():
             qmm._check_block_operand(other, make(per))
     with pytest.raises(ValueError, match="block_operand"):
         qmm._check_block_operand(codes, qmm.BlockOperand(codes.data_ptr(), qmm.E4M3, 1, 0))
+
+
+def test_quantize_blocks_extents(L):
+    """Up to 2^31 - 129 elements along either axis, as the header says (refused before the step sizes' missing place is)."""
+    call = lambda x: L.qmm_quantize_blocks(R(x), qmm.E4M3, 1, 0, 0, 0, None, None, None, None, None)
+    most = 2 ** 31 - 129
+    for axis in (0, 1):
+        assert call(T(rows=most, cols=1, axis=axis)) == NULL and call(T(rows=1, cols=most, axis=axis)) == NULL
+        assert call(T(rows=most + 1, cols=1, axis=axis)) == UNSUPPORTED and call(T(rows=1, cols=most + 1, axis=axis)) == UNSUPPORTED
