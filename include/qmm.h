@@ -455,8 +455,8 @@ qmm_status qmm_dropout(const qmm_tensor* x, float p, uint64_t seed, uint64_t off
  *   y_out         device, dense, x's type: y rounded once, or NULL.   mean_out, rstd_out  device, batch * rows floats, or NULL.
  *   delta_out, codes_out  device, both NULL: no quantization (fmt, block, mode are then not looked at).
  * Random bits of stochastic rounding as in qmm_quantize.  The mean is subtracted before the squares are summed, and what its rounding left is taken out
- * again: a row's offset does not cost its variance's accuracy.  A row whose squares overflow binary32 has rstd 0 and y = bias; a row with an inf or
- * NaN, or whose sum overflows, has y NaN, delta NaN and codes 0x7F (INT8 0).  Where all of a row's differences are zero and eps = 0, its rstd is infinite and y = bias.  cols = 0: delta 1
+ * again: a row's offset does not cost its variance's accuracy.  A row whose squares alone overflow binary32 has rstd 0 and y = bias; a row with an inf or
+ * NaN, or of which a sum or a difference to the mean overflows, has y NaN, delta NaN and codes 0x7F (INT8 0).  Where all of a row's differences are zero and eps = 0, its rstd is infinite and y = bias.  cols = 0: delta 1
  * (block = 0), mean 0, rstd 1 / sqrt(eps).  Uses no workspace.  Errors as for qmm_rmsnorm_quantize; dropout outside 0 to 1: QMM_ERR_SHAPE; block: QMM_ERR_ENUM.
  */
 qmm_status qmm_layernorm_quantize(const qmm_tensor* x, const qmm_tensor* residual, const void* weight, const void* bias, qmm_dtype weight_dtype,
