@@ -351,14 +351,14 @@ struct LayerGradArgs {
     int64_t batch, rows, cols, shares;
 };
 
-template <typename T, bool STREAM> QMM_DEV void store_gradients(const LayerGradArgs& a, int64_t p, const float* v, int left)
+template <typename T> QMM_DEV void store_gradients(const LayerGradArgs& a, int64_t p, const float* v, int left)
 {
     constexpr int V = Vec<T>::V;
-    put_row<T, STREAM>(static_cast<T*>(a.dh) + p, pack_row<T>(v), left);
+    store_row<T>(static_cast<T*>(a.dh) + p, pack_row<T>(v), left);
     if (!a.dx) return;
     float u[V];
     drop_values<V>(a.drop, (uint64_t)p + a.drop.offset, v, u);
-    put_row<T, STREAM>(static_cast<T*>(a.dx) + p, pack_row<T>(u), left);
+    store_row<T>(static_cast<T*>(a.dx) + p, pack_row<T>(u), left);
 }
 
 // A thread's next row is on its way while it works on the current one; workgroups of 1024 threads, whose threads have 128 registers, do without.
@@ -440,7 +440,7 @@ layernorm_grad_rows(LayerGradArgs a)
                 const float n = (Vec<T>::at(row.w[k], e) - row.mean) * rstd;
                 v[e] = fmaf(rstd, fmaf(-n, mean_an, Vec<T>::at(row.g[k], e) * weight[k][e] - mean_a), Vec<T>::at(row.q[k], e));
             }
-            store_gradients<T, false>(a, id * a.cols + c, v, left);
+            store_gradients<T>(a, id * a.cols + c, v, left);
         }
         if constexpr (AHEAD) row = next;
     }
@@ -515,7 +515,7 @@ layernorm_grad_long(LayerGradArgs a)
                 const float n = (Vec<T>::at(w, e) - mean) * rstd;
                 v[e] = fmaf(rstd, fmaf(-n, mean_an, Vec<T>::at(g, e) * weight[e] - mean_a), Vec<T>::at(q, e));
             }
-            store_gradients<T, false>(a, id * a.cols + c, v, cols - c);
+            store_gradients<T>(a, id * a.cols + c, v, cols - c);
         }
     }
 }
