@@ -153,7 +153,7 @@ qmm_status qmm_scale_static(const qmm_tensor* x, qmm_format fmt, const qmm_granu
  *   QMM_ROUND_STOCHASTIC: with lo <= |t| < hi the neighbouring grid values, the
  *   result is hi iff u < (|t|-lo)/(hi-lo), u = (24 random bits)/2^24.  The bits
  *   of output element p (linear index in codes_out) are the top 24 bits of word
- *   (p+offset)%4 of Philox4x32-10 with counter ((p+offset)/4, 0) as two 32-bit
+ *   (p+offset)%4 of Philox4x32-10, p+offset modulo 2^64, with counter ((p+offset)/4, 0) as two 32-bit
  *   halves followed by two zero words, and key = seed as two 32-bit halves, so
  *   a tensor quantized in pieces with matching offsets equals the whole.
  *   codes_out  device, [batch][non-contracting][contracting] bytes, dense: the

@@ -87,7 +87,8 @@ template <int FMT, int MODE, int Q> QMM_DEV void encode_quads(const float (&t)[4
         // offset or the row length is not a multiple of 4), else parts of Q + 1.
         const uint64_t c = g >> 2;
         const uint32_t j = (uint32_t)g & 3u, k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
-        auto block = [&](int q) { return philox4x32_10((uint32_t)(c + q), (uint32_t)((c + q) >> 32), 0u, 0u, k0, k1); };
+        // (behind the last number comes number 0: element counts are modulo 2^64, blocks modulo 2^62)
+        auto block = [&](int q) { return philox4x32_10((uint32_t)(c + q), (uint32_t)((c + q) >> 32) & (q ? 0x3FFFFFFFu : ~0u), 0u, 0u, k0, k1); };
         uint32_t w[4 * Q + 4];
         auto take = [&](int q) {
             const Philox4 p = block(q);

@@ -556,3 +556,29 @@ def test_single_linear_end_to_end(fmt, per_channel):
     # the metric pass itself on identical inputs
     m_same = O.metric(y.cpu().numpy(), r.cpu().numpy())
     assert np.allclose(m, m_same, rtol=1e-10, atol=0)
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 40), (64, 256), (33, 129), (2048, 512), (5000, 72)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_random_numbers_start_again_behind_the_last(rows, cols, dtype):
+    """Element numbers are modulo 2^64, in a vector that holds the last one and the first ones as well: every call that rounds stochastically."""
+    x = torch.randn((rows, cols), generator=torch.Generator().manual_seed(9)).to(dtype)
+    xd, xn = x.to(DEV), np32(x)
+    for back in (1, 2, 3, 5, 6, 7, 9, 11, 14, 15):
+        kw = dict(mode=qmm.STOCHASTIC, seed=back, offset=2 ** 64 - back)
+        for axis in (1, 0):
+            for fmt in (qmm.INT8, qmm.E4M3, qmm.E5M2):
+                step = qmm.scale(xd, axis, fmt)
+                want = O.quantize(xn, axis, fmt, step.cpu().numpy(), **kw)
+                assert np.array_equal(qmm.quantize(xd, axis, fmt, step, **kw).cpu().numpy(), want), (back, axis, fmt)
+                assert np.array_equal(qmm.scale_quantize(xd, axis, fmt, **kw)[0].cpu().numpy(), want), (back, axis, fmt)
+                if fmt != qmm.INT8 and axis == 1:              # the first block of 128 columns (the only one whose numbers are consecutive from the first row on)
+                    c, d = qmm.quantize_blocks(xd, 1, fmt, **kw)
+                    got = O.quantize(xn[:1, :128], 1, fmt, d[0, 0, :1].cpu().numpy(), **kw)
+                    assert np.array_equal(c[0, :1, :128].cpu().numpy(), got[0])
+                    ct, dt = qmm.quantize_blocks(xd, 0, fmt, **kw)
+                    got = O.quantize(xn[:128, :1], 0, fmt, dt[0, 0, :1].cpu().numpy(), **kw)
+                    assert np.array_equal(ct[0, :1, :128].cpu().numpy(), got[0])
+        if dtype == torch.float32:
+            n = qmm.layernorm_quantize(xd, None, None, qmm.E4M3, want_y=True, **kw)
+            assert np.array_equal(n.codes.cpu().numpy(), O.quantize(n.y.cpu().numpy(), 1, qmm.E4M3, n.delta.cpu().numpy(), per_channel=True, **kw))
