@@ -686,7 +686,8 @@ extern "C" qmm_status qmm_layernorm_quantize(const qmm_tensor* x, const qmm_tens
     a.batch = x->batch; a.rows = x->rows; a.cols = x->cols;
     a.seed = seed; a.offset = offset;
     if (codes) { a.qmax = host_qmax(fmt); a.fmt = fmt; }
-    // (as in qmm_rmsnorm_quantize)
+    // As in qmm_rmsnorm_quantize, where a residual is read beside x.  Without one the rule is ordinary loads, though streaming is mostly faster there too (16384 x 4096
+    // bfloat16, dropout and all outputs, 104 us by ordinary loads, 95 by streaming; without dropout 84 / 80; 65536 x 1024, codes alone, 65 / 68).
     const bool streaming = residual && streams(x) && streams(residual) && aligned16(h_out) && aligned16(y_out);
     hipStream_t s = as_stream(stream);
     return x->dtype == QMM_DT_BF16 ? launch_layer_form<uint16_t>(a, block == kBlock, mode, streaming, s) : launch_layer_form<float>(a, block == kBlock, mode, streaming, s);
