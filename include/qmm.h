@@ -418,8 +418,8 @@ typedef struct {
  *   a [batch][M][K], b [batch][N][K]: E4M3 and E5M2 may be mixed, each has its block_rows.  The usual pairs are rows by 128 x 128 blocks of weights, and in a
  *              weight gradient rows by rows; blocks of 128 rows in b are the faster ones.
  *   y          device [batch][M][N], y_dtype F32 or BF16 (RNE), 16-byte aligned.
- *   K a multiple of 16 and at most 2^22, M and N below 2^31, data 16-byte aligned.  Without a contraction (K = 0) y is zero.  More than 2^31 - 1 tiles of 256 x 256 of
- *              y over the batch, or with K = 0 2^24 of 64 x 64: QMM_ERR_UNSUPPORTED.
+ *   K a multiple of 16 and at most 2^22, M and N below 2^31, data 16-byte aligned.  Without a contraction (K = 0) y is zero.  2^31 tiles of 256 x 256 of y and more
+ *              over the batch, or with K = 0 2^24 of 64 x 64: QMM_ERR_UNSUPPORTED.
  *   workspace  qmm_gemm_blocks_workspace_size() bytes, 16-byte aligned (0: may be NULL).  It is non-zero for small outputs with a long K: K is then split
  *              and the parts are added in ascending order.
  */
